@@ -59,7 +59,10 @@ enum {
   MLP_ACT_LINEAR = 0,
   MLP_ACT_RELU = 1,
   MLP_ACT_SIGMOID = 2, /* 1 / (1 + exp(-x)) */
-  MLP_ACT_SINE = 3     /* sin(x) */
+  MLP_ACT_SINE = 3,    /* sin(x) */
+  /* wide layers (mlp_dense_*) only: mlp_create refuses them */
+  MLP_ACT_GELU = 4,    /* x Phi(x), Phi the normal distribution function */
+  MLP_ACT_SILU = 5     /* x / (1 + exp(-x)) */
 };
 
 enum {
@@ -237,6 +240,130 @@ int mlp_adam_step(const mlp_t* h, float* master, float* m, float* v,
                   const float* G, uint16_t* W, void* packed, float lr,
                   float beta1, float beta2, float eps, int64_t t,
                   void* stream);
+
+/* ------------------------------------------------------------------------
+ * Operators around the fused nets (extensions beyond the paper): layer norm,
+ * one layer of any width, and losses over a vocabulary.  They need no
+ * handle.  As everywhere in this library the caller owns every buffer,
+ * nothing is allocated or synchronized, weights are [fan_in][fan_out],
+ * products take bf16 operands and sum in fp32, and each stored bf16 value is
+ * rounded once.  Matrices are row-major with a row stride `ld...` in
+ * elements, from the number of columns to MLP_MAX_DIM; rows may start at any
+ * element (products are fastest when pointers are 16-byte aligned and
+ * dimensions and strides are multiples of 8).  Dimensions other than the
+ * batch are 1 .. MLP_MAX_DIM.  Outputs must not overlap inputs (except
+ * where stated) or the workspace.  Every sum has a fixed order: results are
+ * bitwise the same from run to run.  Workspaces hold nothing between calls;
+ * their size depends on the dimensions and the mode alone, and a call with
+ * gradients needs that of MLP_MODE_TRAIN. */
+
+/* Element types of the arguments named ..._type. */
+enum { MLP_BF16 = 0, MLP_FP32 = 1 };
+
+enum { MLP_MAX_DIM = 1 << 22 };
+
+/* Layer norm of every row: Y = (X - mean) / sqrt(var + eps) gamma + beta, var
+ * the mean square deviation.
+ *   X, Y   [M][N], bf16 or fp32 each; Y may be X where types and strides agree.
+ *   gamma, beta  fp32 [N]; NULL stands for ones and zeros.
+ *   stats  fp32 [M][2], 8-byte aligned, receives mean and 1 / sqrt(var + eps)
+ *          of every row, or NULL.
+ * 0 <= M <= 2^30 (M = 0 enqueues nothing).  eps > 0. */
+int mlp_layer_norm_forward(const void* X, int x_type, int64_t ldx,
+                           const float* gamma, const float* beta, void* Y,
+                           int y_type, int64_t ldy, float* stats, int64_t M,
+                           int64_t N, float eps, void* stream);
+
+/* Workspace of mlp_layer_norm_backward (MLP_MODE_TRAIN; else 0). */
+size_t mlp_layer_norm_workspace_bytes(int64_t M, int64_t N, int mode);
+
+/* Its gradients, from X and the stats that the forward pass wrote.
+ *   dY      [M][N];  dX [M][N], which may be dY where types and strides agree.
+ *   dgamma, dbeta  fp32 [N], sums over the rows (zeros for M = 0).
+ *   ws      256-byte aligned. */
+int mlp_layer_norm_backward(const void* X, int x_type, int64_t ldx,
+                            const float* gamma, const float* stats,
+                            const void* dY, int dy_type, int64_t lddy, void* dX,
+                            int dx_type, int64_t lddx, float* dgamma,
+                            float* dbeta, int64_t M, int64_t N, void* ws,
+                            void* stream);
+
+/* One layer of any width: Y = act(X W + bias) + R.
+ *   X      bf16 [M][K];  W  bf16 [K][N];  bias  fp32 [N] or NULL.
+ *   R      [M][N] of Y's type, or NULL; may be Y itself (same stride).
+ *   Y      [M][N], bf16 or fp32.
+ *   stash  NULL, or fp32 [M][N], contiguous, which receives act'(X W + bias)
+ *          for the backward pass (not touched by a linear layer).  fp32, so
+ *          that the bias's gradient is not that of rounded derivatives.
+ *   ws     mlp_dense_workspace_bytes(M, K, N, MLP_MODE_INFER) bytes, 256-byte
+ *          aligned; may be NULL where that is 0.
+ * 0 <= M <= 2^30 (M = 0 enqueues nothing). */
+int mlp_dense_forward(const uint16_t* X, int64_t ldx, const uint16_t* W,
+                      int64_t ldw, const float* bias, int activation,
+                      const void* R, int64_t ldr, void* Y, int y_type,
+                      int64_t ldy, float* stash, int64_t M, int64_t K,
+                      int64_t N, void* ws, void* stream);
+
+size_t mlp_dense_workspace_bytes(int64_t M, int64_t K, int64_t N, int mode);
+
+/* Its gradients.  dZ = dY act' is rounded to bf16 once (a bf16 dY of a linear
+ * layer is used as it is); R's gradient is dY.
+ *   dY   [M][N], bf16 or fp32.
+ *   dX   [M][K] = dZ W^T, or NULL;  dW  [K][N] = X^T dZ, or NULL.
+ *   db   fp32 [N], the sums over the rows of the unrounded dZ, or NULL.
+ *   ws   mlp_dense_workspace_bytes(M, K, N, MLP_MODE_TRAIN) bytes.
+ * Where ReLU's derivative is 0 the delta is 0 even if dY is not finite.
+ * M = 0: dW and db are zeros. */
+int mlp_dense_backward(const uint16_t* X, int64_t ldx, const uint16_t* W,
+                       int64_t ldw, int activation, const float* stash,
+                       const void* dY, int dy_type, int64_t lddy, void* dX,
+                       int dx_type, int64_t lddx, void* dW, int dw_type,
+                       int64_t lddw, float* db, int64_t M, int64_t K, int64_t N,
+                       void* ws, void* stream);
+
+/* Workspace of mlp_cross_entropy (top = 1) and mlp_distill for M rows of
+ * hidden size D and a vocabulary of V; 1 <= top <= 1024. */
+size_t mlp_head_workspace_bytes(int64_t M, int64_t D, int64_t V, int top,
+                                int mode);
+
+/* Softmax cross entropy of the logits L = H W, which are never stored whole:
+ * the loss keeps a running maximum and sum per row, the gradients recompute
+ * the logits in pieces of the vocabulary (at most 512 MiB of them at a time,
+ * or 1024 columns).
+ *   H       bf16 [M][D];  W  bf16 [D][V].
+ *   target  int64 [M], 8-byte aligned: 0 .. V - 1, or ignore_index for a row
+ *           that does not count.  Any other value makes the loss (and the
+ *           gradients, if asked for) NaN.
+ *   loss    device float or NULL: the mean over the rows that count of
+ *           log sum exp L - L[target] (0 if none does).
+ *   row_loss  fp32 [M] or NULL: the same per row, 0 for rows that do not count.
+ *   dH      [M][D], dW [D][V], bf16 or fp32 each: gradients of the mean loss;
+ *           both or neither (NULL).  softmax - target is rounded to bf16 once
+ *           before the two products.  A row that does not count gives zeros
+ *           to dH; its H has to be finite for dW, as in any product.
+ * 0 <= M <= 2^24. */
+int mlp_cross_entropy(const uint16_t* H, int64_t ldh, const uint16_t* W,
+                      int64_t ldw, const int64_t* target, int64_t ignore_index,
+                      float* loss, float* row_loss, void* dH, int dh_type,
+                      int64_t lddh, void* dW, int dw_type, int64_t lddw,
+                      int64_t M, int64_t D, int64_t V, void* ws, void* stream);
+
+/* Distillation from a teacher's top logits.  With q the softmax of a row's
+ * teacher logits / temperature over its `top` entries and p the softmax of
+ * H W / temperature over the whole vocabulary, a row's loss is
+ * temperature^2 sum q (log q - log p).
+ *   index   int64 [M][top], contiguous: a negative index is no entry, one past
+ *           the vocabulary makes loss and gradients NaN; an index may occur
+ *           twice (its probabilities add up).  A row without an entry (or
+ *           with logits of -inf alone) does not count.
+ *   logits  [M][top], bf16 or fp32, contiguous.
+ * Other arguments as for mlp_cross_entropy. */
+int mlp_distill(const uint16_t* H, int64_t ldh, const uint16_t* W, int64_t ldw,
+                const int64_t* index, const void* logits, int logits_type,
+                int top, float temperature, float* loss, float* row_loss,
+                void* dH, int dh_type, int64_t lddh, void* dW, int dw_type,
+                int64_t lddw, int64_t M, int64_t D, int64_t V, void* ws,
+                void* stream);
 
 /* Description of the last error on this thread ("" if none). */
 const char* mlp_last_error(void);

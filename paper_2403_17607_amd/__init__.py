@@ -13,6 +13,10 @@ Operations (arXiv 2403.17607, section III-A):
                     gradients G_i = A_i^T D_{i+1}, no input gradient.
   * train_step   -- Algorithm 2 with the mean-squared-error loss.
 
+Around them, for nets inside a language model (layers.py): LayerNorm, Dense
+(one layer of any width) and SoftmaxHead (cross entropy and distillation over
+a vocabulary), each with its backward pass.
+
 Example::
 
     net = FusedMLP(width=64, depth=4, in_dim=64, out_dim=16, activation="relu")
@@ -45,6 +49,8 @@ WIDTHS = (16, 32, 64, 128)
 
 # Every exported symbol of include/ffmlp.h with its ctypes signature.
 _VP = ctypes.c_void_p
+_INT = ctypes.c_int
+_I64 = ctypes.c_int64
 _SIGNATURES = {
     "mlp_create": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
                                    ctypes.c_int, ctypes.POINTER(_VP)]),
@@ -69,6 +75,21 @@ _SIGNATURES = {
                                      ctypes.c_float, ctypes.c_float, ctypes.c_float,
                                      ctypes.c_int64, _VP]),
     "mlp_last_error": (ctypes.c_char_p, []),
+    "mlp_layer_norm_workspace_bytes": (ctypes.c_size_t, [_I64, _I64, _INT]),
+    "mlp_layer_norm_forward": (_INT, [_VP, _INT, _I64, _VP, _VP, _VP, _INT, _I64, _VP, _I64, _I64,
+                                      ctypes.c_float, _VP]),
+    "mlp_layer_norm_backward": (_INT, [_VP, _INT, _I64, _VP, _VP, _VP, _INT, _I64, _VP, _INT, _I64,
+                                       _VP, _VP, _I64, _I64, _VP, _VP]),
+    "mlp_dense_workspace_bytes": (ctypes.c_size_t, [_I64, _I64, _I64, _INT]),
+    "mlp_dense_forward": (_INT, [_VP, _I64, _VP, _I64, _VP, _INT, _VP, _I64, _VP, _INT, _I64, _VP,
+                                 _I64, _I64, _I64, _VP, _VP]),
+    "mlp_dense_backward": (_INT, [_VP, _I64, _VP, _I64, _INT, _VP, _VP, _INT, _I64, _VP, _INT, _I64,
+                                  _VP, _INT, _I64, _VP, _I64, _I64, _I64, _VP, _VP]),
+    "mlp_head_workspace_bytes": (ctypes.c_size_t, [_I64, _I64, _I64, _INT, _INT]),
+    "mlp_cross_entropy": (_INT, [_VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _VP, _INT, _I64, _VP,
+                                 _INT, _I64, _I64, _I64, _I64, _VP, _VP]),
+    "mlp_distill": (_INT, [_VP, _I64, _VP, _I64, _VP, _VP, _INT, _INT, ctypes.c_float, _VP, _VP,
+                           _VP, _INT, _I64, _VP, _INT, _I64, _I64, _I64, _I64, _VP, _VP]),
 }
 
 _lib = None
@@ -347,3 +368,7 @@ class FusedMLP:
         _check(lib().mlp_train_step_noalloc(self._h, _ptr(packed), _ptr(X), _ptr(T), _ptr(Y),
                                             _ptr(G), _ptr(loss), M, _stream(dev)))
         return G, loss
+
+
+from .layers import (ACTIVATIONS_DENSE, MLP_BF16, MLP_FP32, MLP_MAX_DIM, Dense, LayerNorm,  # noqa: E402,F401
+                     SoftmaxHead)

@@ -22,7 +22,9 @@ SOURCES = ["api.hip", "fwd.hip", "fwd16.hip", "fwd32.hip", "fwd64.hip", "fwd64u.
            "fwd128.hip", "fwd128u.hip", "bwdg.hip", "bwdg64.hip", "bwdg128.hip",
            "bwd.hip", "bwd16.hip", "bwd32.hip", "bwd64.hip", "bwd128.hip", "wgrad.hip",
            "bwds.hip", "bwds16.hip", "bwds32.hip", "bwds64.hip", "bwds128.hip",
-           "trainf.hip", "trainf16.hip", "trainf32.hip", "trainf64.hip", "reduce.hip", "optim.hip"]
+           "trainf.hip", "trainf16.hip", "trainf32.hip", "trainf64.hip", "reduce.hip", "optim.hip",
+           "layers.hip", "norm.hip", "gemm.hip", "gemm_xw.hip", "gemm_dx.hip", "gemm_dw.hip",
+           "head.hip", "head_ce.hip", "head_distill.hip"]
 # The longest compilations, started first so that none runs on alone at the end.
 SLOW = ["trainf64.hip", "fwd64u.hip", "fwd128u.hip", "fwd64.hip", "fwd128.hip", "trainf32.hip", "fwd32.hip", "fwd16.hip",
         "bwds128.hip"]

@@ -12,6 +12,7 @@
 
 #include "common.h"
 #include "ffmlp.h"
+#include "host.h"
 
 using namespace ffmlp;
 
@@ -20,10 +21,11 @@ struct mlp {
 };
 
 namespace {
-
 thread_local std::string g_err;
+}
 
-int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+namespace ffmlp {
+
 int fail(int code, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -38,9 +40,11 @@ int hip_fail(hipError_t e, const char* what) {
   return fail(MLP_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+void clear_error() { g_err.clear(); }
 
-size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+}  // namespace ffmlp
+
+namespace {
 
 int n_mats(const mlp* h) { return h->depth + 1; }
 int fan_in_of(const mlp* h, int l) { return l == 0 ? h->in_dim : h->width; }

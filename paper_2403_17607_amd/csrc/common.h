@@ -54,7 +54,8 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-enum { ACT_LINEAR = 0, ACT_RELU = 1, ACT_SIGMOID = 2, ACT_SINE = 3 };
+enum { ACT_LINEAR = 0, ACT_RELU = 1, ACT_SIGMOID = 2, ACT_SINE = 3,
+       ACT_GELU = 4, ACT_SILU = 5 };  // the last two: wide layers only
 
 // Rows per workgroup tile in the fused forward and backward kernels:
 // NT 16-row blocks per wave, NW waves per workgroup.

@@ -1,0 +1,438 @@
+// Matrix products of any size on the matrix cores, C = A B with bf16 operands
+// and fp32 sums, as the wide layers and the vocabulary losses use them.
+//
+// The m side (rows of C) and the n side (columns of C) are each a row-major
+// matrix, either with the contracted index k along its rows (T = false:
+// [m][k], [n][k]) or across them (T = true: [k][m], [k][n]):
+//     Y  = X W      X [m][k]  W [k][n]     m false, n true
+//     dX = dZ W^T   dZ [m][k] W [n][k]     m false, n false
+//     dW = X^T dZ   X [k][m]  dZ [k][n]    m true,  n true
+// A workgroup owns a BM x BN tile of C and walks k in steps of BK.  Each step
+// brings a BK slice of both sides to LDS as it lies in memory; a side with k
+// across its rows is transposed by the LDS read (ds_read_b64_tr_b16: 16 lanes
+// read a 4 x 16 block and lane i gets its column i), so no operand is
+// repacked.  The n side is the first MFMA operand: lane (i, g) of the result
+// holds four consecutive columns 4 g .. 4 g + 3 of row i.
+//
+// LDS holds 16-byte pieces, [row][piece], the piece index XORed with a
+// function of the row (below) so that the reads hit every bank once.
+#pragma once
+
+#include "device.h"
+#include "gemm.h"
+
+namespace ffmlp {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// One workgroup tile: BM x BN of C, WM x WN waves, BK of k per step, ST LDS
+// buffers.
+template <int BM_, int BN_, int BK_, int WM_, int WN_, int ST_>
+struct GemmTile {
+  static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, ST = ST_;
+  static constexpr int NW = WM * WN, NTHR = NW * 64;
+  static constexpr int MB = BM / WM / 16, NB = BN / WN / 16;  // 16 x 16 blocks of a wave
+};
+
+// One side's slice of a step: R rows or columns of C by BK of k.
+template <bool T, int R, int BK, int NTHR>
+struct Side {
+  static constexpr int ROWS = T ? BK : R;        // rows of the slice in LDS
+  static constexpr int CH = (T ? R : BK) / 8;    // 16-byte pieces of a row
+  static constexpr int PIECES = ROWS * CH;
+  static constexpr int PER = (PIECES + NTHR - 1) / NTHR;  // pieces a thread loads
+  static constexpr int BYTES = PER * NTHR * 16;           // whole loads of the workgroup
+  // Piece permutation of a row.  k along the rows: eight lanes read the same
+  // piece of eight rows (128 bytes of banks).  k across: 16 lanes read 32
+  // bytes of four rows, 32 lanes of rows r .. r + 3 and r + 8 .. r + 11.
+  static __device__ __forceinline__ int swz(int row) {
+    if constexpr (T) return (2 * ((row & 3) + 4 * ((row >> 3) & 1))) & (CH - 1);
+    else if constexpr (CH >= 8) return row & 7;
+    else return (row >> 1) & 3;
+  }
+};
+
+// The global side of the loads of one thread, for a workgroup that owns the
+// rows (T = false) or columns (T = true) from r0 on and contracts k0 .. kend - 1.
+template <typename S, bool T, int BK, int NTHR, bool DIRECT>
+struct Loader {
+  SideArgs a;
+  int64_t r0, kend;
+  const uint8_t* p;       // direct loads: the next step's first element,
+  int64_t left;           //   the bytes from it to the end of what may be read
+  int krem;               //   and the k from it on
+  uint32_t voff[S::PER];  // byte offsets of the thread's pieces within a step
+  u32x4 v[DIRECT ? 1 : S::PER];
+
+  static __device__ __forceinline__ int piece_row(int j, int tid) { return (j * NTHR + tid) / S::CH; }
+  static __device__ __forceinline__ int piece_col(int j, int tid) {
+    return 8 * (((j * NTHR + tid) % S::CH) ^ S::swz(piece_row(j, tid)));
+  }
+  static __device__ __forceinline__ bool piece_in(int j, int tid) {
+    return S::PER * NTHR == S::PIECES || j * NTHR + tid < S::PIECES;
+  }
+
+  __device__ __forceinline__ void init(const SideArgs& args, int64_t first, int64_t k0, int64_t k1, int tid) {
+    a = args;
+    r0 = first;
+    kend = k1;
+    if constexpr (DIRECT) {
+      const int64_t row = T ? k0 : r0, col = T ? r0 : k0, last = T ? k1 - 1 : a.rows - 1;
+      p = reinterpret_cast<const uint8_t*>(a.p + row * a.ld + col);
+      left = ((last - row) * a.ld + a.cols - col) * 2;
+      krem = (int)(k1 - k0);
+#pragma unroll
+      for (int j = 0; j < S::PER; ++j)
+        voff[j] = piece_in(j, tid) ? (uint32_t)(((int64_t)piece_row(j, tid) * a.ld + piece_col(j, tid)) * 2) : kOOB;
+    }
+  }
+  // The next step to LDS at `lds` without passing through registers.  Pieces
+  // past kend or past the matrix are out of the descriptor's range and arrive
+  // as zeros, so steps past the last one may be loaded too.  What follows a
+  // T side's row in memory comes along in its last tile: it only reaches
+  // columns of C that do not exist.
+  __device__ __forceinline__ void to_lds(uint32_t lds, int wave, int tid) {
+    // (a buffer descriptor as make_rsrc builds it, in scalar registers)
+    const uint64_t at = (uint64_t)p;
+    const int64_t n = krem <= 0 || left <= 0 ? 0 : (left > 0x7fffffff ? 0x7fffffff : left);
+    const u32x4 r = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)n, 0x00020000u};
+#pragma unroll
+    for (int j = 0; j < S::PER; ++j) {
+      uint32_t o = voff[j];
+      if (!T) o = piece_col(j, tid) < krem ? o : kOOB;
+      const uint32_t dst = lds + (uint32_t)(j * NTHR + wave * 64) * 16;
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                   :: "s"(dst), "v"(o), "s"(r) : "memory");
+    }
+    const int64_t step = T ? a.ld * (BK * 2) : BK * 2;
+    p += step;
+    left -= step;
+    krem -= BK;
+  }
+  // The pieces of the step from k0 on through registers, for matrices whose
+  // rows start anywhere: unaligned 16-byte loads, the last piece of a row by
+  // element.
+  __device__ __forceinline__ void to_regs(int64_t k0, int tid) {
+    const int64_t rend = T ? kend : a.rows, cend = T ? a.cols : kend;
+#pragma unroll
+    for (int j = 0; j < S::PER; ++j) {
+      const int64_t row = (T ? k0 : r0) + piece_row(j, tid), c = (T ? r0 : k0) + piece_col(j, tid);
+      u32x4 x = {0u, 0u, 0u, 0u};
+      if (piece_in(j, tid) && row < rend && c < cend) {
+        const uint16_t* src = a.p + row * a.ld + c;
+        if (c + 8 <= cend) {
+          x = *reinterpret_cast<const u32x4_a2*>(src);
+        } else {
+          uint32_t e[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) e[q] = c + q < cend ? (uint32_t)src[q] : 0u;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) x[q] = e[2 * q] | (e[2 * q + 1] << 16);
+        }
+      }
+      v[j] = x;
+    }
+  }
+  __device__ __forceinline__ void regs_to_lds(uint8_t* lds, int tid) const {
+#pragma unroll
+    for (int j = 0; j < S::PER; ++j) *reinterpret_cast<u32x4*>(lds + (j * NTHR + tid) * 16) = v[j];
+  }
+};
+
+// A wave's operand fragments of one 32-wide block of k: block b holds rows
+// (columns of C) w0 + 16 b + i, lane group g the positions 8 g .. 8 g + 7.
+template <typename S, bool T, int NBLK>
+struct Frags {
+  uint32_t at[T ? NBLK : S::CH / 4];  // LDS byte offsets within the slice
+  __device__ __forceinline__ void init(int w0, int lane) {
+    const int i = lane & 15, g = lane >> 4;
+    if constexpr (T) {
+      const int row = 8 * g + (i >> 2), h = S::swz(row);
+#pragma unroll
+      for (int b = 0; b < NBLK; ++b) {
+        const int piece = (w0 + 16 * b) / 8 + ((i & 3) >> 1);
+        at[b] = (uint32_t)((row * S::CH + (piece ^ h)) * 16 + 8 * (i & 1));
+      }
+    } else {
+      const int row = w0 + i;
+#pragma unroll
+      for (int kk = 0; kk < S::CH / 4; ++kk) at[kk] = (uint32_t)((row * S::CH + ((4 * kk + g) ^ S::swz(row))) * 16);
+    }
+  }
+  // Block b of k-block kk; lds: the slice's first byte.
+  __device__ __forceinline__ u32x4 read(const uint8_t* lds, int kk, int b) const {
+    if constexpr (T) {
+      typedef s16x4 __attribute__((address_space(3))) lds_s16x4;
+      // rows + 4 keep swz(row) (it does not look at bit 2)
+      const uint8_t* p = lds + at[b] + kk * 32 * S::CH * 16;
+      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
+      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * S::CH * 16)));
+      return u32x4{lo[0], lo[1], hi[0], hi[1]};
+    } else {
+      return *reinterpret_cast<const u32x4*>(lds + at[kk] + b * 16 * S::CH * 16);
+    }
+  }
+};
+
+// Waits for all but the newest N of the wave's direct loads and for its LDS
+// reads, then for the workgroup.
+template <int N>
+__device__ __forceinline__ void wait_loads_barrier() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(N) : "memory");
+}
+
+// acc += the BM x BN tile's products over k in [k0, k1), k0 a multiple of BK.
+// `lds`: the workgroup's ST buffers of the two slices.  Every wave passes the
+// last barrier only after its own reads, so the buffers are free afterwards
+// once the caller has synchronized.
+template <typename TL, bool MT, bool NT, bool DIRECT>
+__device__ __forceinline__ void gemm_loop(const SideArgs& ma, const SideArgs& na, int64_t m0, int64_t n0, int64_t k0,
+                                          int64_t k1, uint8_t* lds, f32x4 (&acc)[TL::MB][TL::NB]) {
+  typedef Side<MT, TL::BM, TL::BK, TL::NTHR> SM;
+  typedef Side<NT, TL::BN, TL::BK, TL::NTHR> SN;
+  constexpr int STAGE = SM::BYTES + SN::BYTES;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / TL::WN, wn = wave % TL::WN;
+  Loader<SM, MT, TL::BK, TL::NTHR, DIRECT> lm;
+  Loader<SN, NT, TL::BK, TL::NTHR, DIRECT> ln;
+  lm.init(ma, m0, k0, k1, tid);
+  ln.init(na, n0, k0, k1, tid);
+  Frags<SM, MT, TL::MB> fm;
+  Frags<SN, NT, TL::NB> fn;
+  fm.init(wm * TL::MB * 16, lane);
+  fn.init(wn * TL::NB * 16, lane);
+  const int nk = (int)((k1 - k0 + TL::BK - 1) / TL::BK);
+  auto multiply = [&](const uint8_t* s) {
+#pragma unroll
+    for (int kk = 0; kk < TL::BK / 32; ++kk) {
+      u32x4 b[TL::NB];
+#pragma unroll
+      for (int n = 0; n < TL::NB; ++n) b[n] = fn.read(s + SM::BYTES, kk, n);
+#pragma unroll
+      for (int m = 0; m < TL::MB; ++m) {
+        const u32x4 a = fm.read(s, kk, m);
+#pragma unroll
+        for (int n = 0; n < TL::NB; ++n) acc[m][n] = mfma16(b[n], a, acc[m][n]);
+      }
+    }
+  };
+  if constexpr (DIRECT) {
+    constexpr int LOADS = SM::PER + SN::PER;
+    const uint32_t l0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+    auto issue = [&](int slot) {
+      lm.to_lds(l0 + slot * STAGE, wave, tid);
+      ln.to_lds(l0 + slot * STAGE + SM::BYTES, wave, tid);
+    };
+#pragma unroll
+    for (int t = 0; t < TL::ST - 1; ++t) issue(t);
+    int slot = 0;
+    for (int t = 0; t < nk; ++t) {
+      wait_loads_barrier<(TL::ST - 2) * LOADS>();
+      // into the buffer of step t - 1, which every wave has read.  Steps past
+      // the last load zeros, so that the count of loads in flight stays the same.
+      issue(slot == 0 ? TL::ST - 1 : slot - 1);
+      multiply(lds + slot * STAGE);
+      slot = slot + 1 == TL::ST ? 0 : slot + 1;
+    }
+    wait_loads_barrier<0>();
+  } else {
+    lm.to_regs(k0, tid);
+    ln.to_regs(k0, tid);
+    lm.regs_to_lds(lds, tid);
+    ln.regs_to_lds(lds + SM::BYTES, tid);
+    for (int t = 0; t < nk; ++t) {
+      __syncthreads();
+      const int64_t k = k0 + (int64_t)(t + 1) * TL::BK;
+      if (k < k1) {
+        lm.to_regs(k, tid);
+        ln.to_regs(k, tid);
+      }
+      multiply(lds + (t & 1) * STAGE);
+      if (k < k1) {
+        lm.regs_to_lds(lds + (~t & 1) * STAGE, tid);
+        ln.regs_to_lds(lds + (~t & 1) * STAGE + SM::BYTES, tid);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+template <typename TL, bool MT, bool NT, bool DIRECT>
+constexpr int gemm_lds_bytes() {
+  constexpr int loop = (DIRECT ? TL::ST : 2) *
+                       (Side<MT, TL::BM, TL::BK, TL::NTHR>::BYTES + Side<NT, TL::BN, TL::BK, TL::NTHR>::BYTES);
+  constexpr int out = TL::NW * 16 * (TL::NB * 16 + 4) * 4;  // the results of one 16-row block of each wave
+  return loop > out ? loop : out;
+}
+
+// Tile `t` of mt x nt, in an order that keeps a chiplet's tiles together: the
+// hardware deals workgroups out to the eight chiplets in turn, each with its
+// own L2, so workgroup b takes tile (b % 8) of eight equal runs; within the
+// order, groups of eight tile rows share the n side's tiles.
+__device__ __forceinline__ void gemm_tile_of(int b, int mt, int nt, int& tm, int& tn) {
+  const int total = mt * nt, q = total / 8, r = total % 8, x = b % 8, y = b / 8;
+  const int t = x * q + (x < r ? x : r) + y;
+  constexpr int G = 8;
+  const int per = G * nt, grp = t / per, first = grp * G;
+  const int rows = mt - first < G ? mt - first : G;
+  const int in = t - grp * per;
+  tm = first + in % rows;
+  tn = in / rows;
+}
+
+// act(z) in y and act'(z) in d.  GELU is z Phi(z) with Phi from the rational
+// approximation 7.1.26 of Abramowitz and Stegun (error of erf up to 1.5e-7),
+// whose exponential the derivative needs too.
+__device__ __forceinline__ void act_and_grad(int act, float z, float& y, float& d) {
+  switch (act) {
+    case ACT_RELU: y = z > 0.f ? z : (z != z ? z : 0.f); d = z > 0.f ? 1.f : 0.f; break;
+    case ACT_SIGMOID: y = __builtin_amdgcn_rcpf(1.f + __expf(-z)); d = y * (1.f - y); break;
+    case ACT_SINE: y = __sinf(z); d = __cosf(z); break;
+    case ACT_GELU: {
+      const float e = __expf(-0.5f * z * z), t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * 0.70710678f * __builtin_fabsf(z));
+      const float q = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+      const float phi = z < 0.f ? q : 1.f - q;
+      y = z * phi;
+      d = phi + z * e * 0.39894228f;
+      break;
+    }
+    case ACT_SILU: {
+      const float p = __builtin_amdgcn_rcpf(1.f + __expf(-z));
+      y = z * p;
+      d = p + y * (1.f - p);
+      break;
+    }
+    default: y = z; d = 1.f;
+  }
+}
+
+// Four columns n .. n + 3 of row m of a product's result, as `o` says.
+__device__ __forceinline__ void out4(const GemmOut& o, int64_t m, int n, int N, f32x4 z) {
+  const bool vec = o.vec && n + 4 <= N;
+  if (o.add) {
+    const float* p = o.add + m * o.ldadd + n;
+    if (vec) z += *reinterpret_cast<const f32x4*>(p);
+    else
+#pragma unroll
+      for (int q = 0; q < 4; ++q) if (n + q < N) z[q] += p[q];
+  }
+  if (o.alpha) z *= *o.alpha;
+  if (o.bias) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) z[q] += o.bias[n + q < N ? n + q : N - 1];
+  }
+  if (o.act != ACT_LINEAR || o.stash) {
+    float d[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float y;
+      act_and_grad(o.act, z[q], y, d[q]);
+      z[q] = y;
+    }
+    if (o.stash) {
+      float* p = o.stash + m * (int64_t)N + n;
+      if (vec) *reinterpret_cast<f32x4*>(p) = f32x4{d[0], d[1], d[2], d[3]};
+      else
+#pragma unroll
+        for (int q = 0; q < 4; ++q) if (n + q < N) p[q] = d[q];
+    }
+  }
+  if (o.c_fp32) {
+    float* p = static_cast<float*>(o.C) + m * o.ldc + n;
+    if (o.R) {
+      const float* r = static_cast<const float*>(o.R) + m * o.ldr + n;
+      if (vec) z += *reinterpret_cast<const f32x4*>(r);
+      else
+#pragma unroll
+        for (int q = 0; q < 4; ++q) if (n + q < N) z[q] += r[q];
+    }
+    if (vec) *reinterpret_cast<f32x4*>(p) = z;
+    else
+#pragma unroll
+      for (int q = 0; q < 4; ++q) if (n + q < N) p[q] = z[q];
+  } else {
+    uint16_t* p = static_cast<uint16_t*>(o.C) + m * o.ldc + n;
+    if (o.R) {
+      const uint16_t* r = static_cast<const uint16_t*>(o.R) + m * o.ldr + n;
+      if (vec) {
+        const u32x2 u = *reinterpret_cast<const u32x2*>(r);
+        z += f32x4{bf16_lo(u[0]), bf16_hi(u[0]), bf16_lo(u[1]), bf16_hi(u[1])};
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) if (n + q < N) z[q] += __uint_as_float((uint32_t)r[q] << 16);
+      }
+    }
+    const u32x2 u = {pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])};
+    if (vec) *reinterpret_cast<u32x2*>(p) = u;
+    else
+#pragma unroll
+      for (int q = 0; q < 4; ++q) if (n + q < N) p[q] = (uint16_t)(u[q / 2] >> (16 * (q & 1)));
+  }
+}
+
+// C = the product, or one split's share of it as fp32 partial sums.
+template <typename TL, bool MT, bool NT, bool DIRECT>
+__global__ __launch_bounds__(TL::NTHR, 2) void gemm_kernel(const GemmArgs a) {
+  extern __shared__ __align__(16) uint8_t gemm_lds[];
+  const int b = blockIdx.x % a.tiles, split = blockIdx.x / a.tiles;
+  int tm, tn;
+  gemm_tile_of(b, a.mt, a.nt, tm, tn);
+  const int64_t m0 = (int64_t)tm * TL::BM;
+  const int n0 = tn * TL::BN;
+  const int64_t k0 = split * a.kper, k1 = k0 + a.kper < a.K ? k0 + a.kper : a.K;
+  f32x4 acc[TL::MB][TL::NB];
+#pragma unroll
+  for (int m = 0; m < TL::MB; ++m)
+#pragma unroll
+    for (int n = 0; n < TL::NB; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  gemm_loop<TL, MT, NT, DIRECT>(a.m, a.n, m0, n0, k0, k1, gemm_lds, acc);
+  GemmOut o = a.out;
+  if (a.splits > 1) {
+    o = GemmOut{};
+    o.C = a.partial + (int64_t)split * a.M * a.N;
+    o.ldc = a.N;
+    o.c_fp32 = 1;
+    o.vec = (a.N & 3) == 0;
+  }
+  // Through LDS, 16 rows of a wave at a time (its own part, so no barrier), so
+  // that a wave's stores cover whole rows of its columns.  Row stride + 4
+  // floats: eight lanes write eight rows' 16 bytes to different banks.
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int COLS = TL::NB * 16, LD = COLS + 4, LPR = COLS / 4, RPI = 64 / LPR;
+  float* part = reinterpret_cast<float*>(gemm_lds) + wave * 16 * LD;
+  const int64_t mw = m0 + (wave / TL::WN) * TL::MB * 16;
+  const int nw = n0 + (wave % TL::WN) * COLS;
+  static_for<0, TL::MB>([&](auto mc) {
+    constexpr int m = decltype(mc)::value;
+#pragma unroll
+    for (int n = 0; n < TL::NB; ++n)
+      *reinterpret_cast<f32x4*>(part + (lane & 15) * LD + 16 * n + 4 * (lane >> 4)) = acc[m][n];
+    __builtin_amdgcn_wave_barrier();
+    const int n = nw + 4 * (lane % LPR);
+#pragma unroll 1
+    for (int r = lane / LPR; r < 16; r += RPI) {
+      const int64_t row = mw + 16 * m + r;
+      if (row < a.M && n < a.N) out4(o, row, n, a.N, *reinterpret_cast<const f32x4*>(part + r * LD + 4 * (lane % LPR)));
+    }
+    __builtin_amdgcn_wave_barrier();
+  });
+}
+
+template <typename TL, bool MT, bool NT, bool DIRECT>
+hipError_t launch_gemm_tile(GemmArgs a, hipStream_t s) {
+  constexpr int lds = gemm_lds_bytes<TL, MT, NT, DIRECT>();
+  const auto k = gemm_kernel<TL, MT, NT, DIRECT>;
+  int occ;
+  const hipError_t e = kernel_occupancy(reinterpret_cast<const void*>(k), TL::NTHR, lds, &occ);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k, dim3((unsigned)(a.tiles * a.splits)), dim3(TL::NTHR), lds, s, a);
+  return hipGetLastError();
+}
+
+// Workgroup tiles.  Large: two workgroups per CU (72 KiB of LDS each), so
+// that one's epilogue and first loads hide behind the other's products.
+typedef GemmTile<128, 256, 32, 2, 2, 3> GemmLarge;
+typedef GemmTile<64, 128, 64, 2, 2, 3> GemmMedium;
+typedef GemmTile<16, 128, 64, 1, 4, 4> GemmRows;
+
+}  // namespace ffmlp

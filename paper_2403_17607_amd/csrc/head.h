@@ -1,0 +1,87 @@
+// Arguments and launches of the vocabulary losses (head_kernel.h, head.hip).
+#pragma once
+
+#include "gemm.h"
+
+namespace ffmlp {
+
+constexpr int kHeadKey = 128;     // columns per entry of the table of starts
+constexpr int kHeadMaxTop = 1024; // teacher entries of a row
+
+struct HeadArgs {
+  SideArgs h, w;          // H [M][D]; W [D][V], or the piece's columns of it
+  int64_t M, D;
+  int V;                  // columns: the vocabulary, or the piece
+  int col0;               // first column of the piece
+  float scale2;           // log2(e) / T
+  // cross entropy: one target per row
+  const int64_t* target;
+  int64_t ignore;
+  // distillation: a row's entries sorted by index
+  const int* index;       // [M][top], absent ones last
+  const float* q;         // [M][top] teacher probabilities
+  const uint16_t* start;  // [M][keys]: entries with index < 128 k
+  int top, keys;
+  float* pick;            // [M][top] logits (base 2) of the entries
+  f32x2* partial;         // [runs * 2][M] maximum and sum
+  int runs, per_run, mt, nt;
+  const float* lse2;      // [M]; +inf: the row does not count
+  uint16_t* P;            // [M][ldp]
+  int64_t ldp;
+};
+
+struct HeadPlan {
+  bool large;
+  int mt, nt, runs, per_run;  // head_lse_kernel
+  int piece, pieces;          // columns of P, a multiple of 256 unless one piece holds all
+};
+HeadPlan head_plan(int64_t M, int64_t D, int64_t V);
+
+hipError_t launch_head_ce(bool prob, bool large, bool direct, const HeadArgs& a, hipStream_t s);
+hipError_t launch_head_distill(bool prob, bool large, bool direct, const HeadArgs& a, hipStream_t s);
+
+// The teacher's entries: probabilities over a row's list, sorted by index,
+// and the table of starts.  ok[m]: 1, 0 (an empty list) or -1 (an index past
+// the vocabulary).
+struct TeacherArgs {
+  const int64_t* index;  // [M][top], negative: absent
+  const void* logits;    // [M][top]
+  int logits_fp32;
+  float inv_t;
+  int64_t M, V;
+  int top, keys;
+  int* out_index;
+  float* out_q;
+  uint16_t* start;
+  int* ok;
+};
+hipError_t launch_teacher(const TeacherArgs& a, hipStream_t s);
+
+// lse2 and the loss of every row, then the mean loss and the gradient's scale.
+struct RowLossArgs {
+  const f32x2* partial;
+  int parts;
+  const float* pick;
+  const float* q;         // null: cross entropy
+  const int* ok;          // distillation
+  const int64_t* target;  // cross entropy
+  int64_t ignore;
+  int top;
+  float t2;               // T^2
+  float temperature;
+  int64_t M, V;
+  float *lse2, *row_loss;
+  float *loss, *alpha;    // mean loss; T / rows that count
+};
+hipError_t launch_row_loss(const RowLossArgs& a, hipStream_t s);
+
+#ifdef __HIPCC__
+// (m, s) and (m2, s2), each a maximum and a sum of 2^(x - maximum), as one.
+__device__ __forceinline__ void head_merge(float& m, float& s, float m2, float s2) {
+  const float top = __builtin_fmaxf(m, m2), at = top == -__builtin_inff() ? 0.f : top;
+  s = s * __builtin_amdgcn_exp2f(m - at) + s2 * __builtin_amdgcn_exp2f(m2 - at);
+  m = top;
+}
+#endif
+
+}  // namespace ffmlp

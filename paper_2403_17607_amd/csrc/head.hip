@@ -1,0 +1,170 @@
+// Vocabulary losses: the plan, the teacher's lists, and the losses of the rows.
+#include "head_kernel.h"
+
+namespace ffmlp {
+
+namespace {
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int64_t kPieceElems = (int64_t)1 << 28;  // P of a piece: 512 MiB
+}  // namespace
+
+HeadPlan head_plan(int64_t M, int64_t, int64_t V) {
+  HeadPlan p{};
+  p.large = cdiv(M, GemmLarge::BM) * cdiv(V, GemmLarge::BN) >= 128;
+  p.mt = (int)cdiv(M, p.large ? GemmLarge::BM : GemmMedium::BM);
+  p.nt = (int)cdiv(V, p.large ? GemmLarge::BN : GemmMedium::BN);
+  int64_t runs = 512 / (p.mt > 0 ? p.mt : 1);
+  if (runs > p.nt) runs = p.nt;
+  if (runs < 1) runs = 1;
+  p.per_run = (int)cdiv(p.nt, runs);
+  p.runs = (int)cdiv(p.nt, p.per_run);
+  int64_t cols = kPieceElems / (M > 0 ? M : 1) / 256 * 256;
+  if (cols < 1024) cols = 1024;
+  const int64_t pieces = cdiv(V, cols);
+  p.piece = (int)(pieces <= 1 ? V : cdiv(cdiv(V, pieces), 256) * 256);
+  p.pieces = (int)cdiv(V, p.piece);
+  return p;
+}
+
+// One wave per row.  The list is sorted by counting, for every entry, the
+// entries before it (index, then position): lists are short, and equal
+// indexes keep their order.
+__global__ __launch_bounds__(64) void teacher_kernel(const TeacherArgs a) {
+  __shared__ int idx[kHeadMaxTop], sorted[kHeadMaxTop];
+  const int64_t row = blockIdx.x;
+  const int lane = threadIdx.x;
+  const int64_t at = row * a.top;
+  auto logit = [&](int e) {
+    const float z = a.logits_fp32 ? static_cast<const float*>(a.logits)[at + e]
+                                  : __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.logits)[at + e] << 16);
+    return z * a.inv_t;
+  };
+  float mx = -__builtin_inff();
+  int bad = 0;
+  for (int e = lane; e < a.top; e += 64) {
+    const int64_t i = a.index[at + e];
+    bad |= i >= a.V;
+    idx[e] = i < 0 || i >= a.V ? 0x7fffffff : (int)i;
+    if (i >= 0) {
+      const float z = logit(e);
+      mx = z != z || mx != mx ? __builtin_nanf("") : __builtin_fmaxf(mx, z);
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const float o = __shfl_xor(mx, d);
+    mx = o != o || mx != mx ? __builtin_nanf("") : __builtin_fmaxf(mx, o);
+    bad |= __shfl_xor(bad, d);
+  }
+  const bool empty = mx == -__builtin_inff();
+  float sum = 0.f;
+  for (int e = lane; e < a.top; e += 64)
+    if (a.index[at + e] >= 0 && !empty) sum += __expf(logit(e) - mx);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+  __syncthreads();
+  for (int e = lane; e < a.top; e += 64) {
+    const int me = idx[e];
+    int rank = 0;
+    for (int o = 0; o < a.top; ++o) rank += idx[o] < me || (idx[o] == me && o < e);
+    sorted[rank] = me;
+    a.out_index[at + rank] = me;
+    a.out_q[at + rank] = me != 0x7fffffff && !empty ? __expf(logit(e) - mx) / sum : 0.f;
+  }
+  __syncthreads();
+  for (int k = lane; k < a.keys; k += 64) {
+    const int64_t first = (int64_t)k * kHeadKey;
+    int lo = 0, hi = a.top;
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (sorted[mid] != 0x7fffffff && sorted[mid] < first) lo = mid + 1; else hi = mid;
+    }
+    a.start[row * a.keys + k] = (uint16_t)lo;
+  }
+  if (lane == 0) a.ok[row] = bad ? -1 : empty ? 0 : 1;
+}
+
+hipError_t launch_teacher(const TeacherArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(teacher_kernel, dim3((unsigned)a.M), dim3(64), 0, s, a);
+  return hipGetLastError();
+}
+
+// One wave per row: its partial sums merged in a fixed tree, then its loss.
+__global__ __launch_bounds__(256) void row_loss_kernel(const RowLossArgs a) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (row >= a.M) return;
+  float m = -__builtin_inff(), s = 0.f;
+  for (int p = lane; p < a.parts; p += 64) {
+    const f32x2 v = a.partial[(int64_t)p * a.M + row];
+    head_merge(m, s, v[0], v[1]);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) head_merge(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
+  float lse = m + __builtin_amdgcn_logf(s), loss = 0.f;  // logf: base 2
+  int state;  // 1 counts, 0 does not, -1 has an index past the vocabulary
+  if (a.q) {
+    state = a.ok[row];
+    for (int e = lane; e < a.top; e += 64) {
+      const float q = a.q[row * a.top + e];
+      if (!(q == 0.f)) loss += q * (kLn2 * (lse - a.pick[row * a.top + e] + __builtin_amdgcn_logf(q)));
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) loss += __shfl_xor(loss, d);
+    loss *= a.t2;
+  } else {
+    const int64_t t = a.target[row];
+    state = t == a.ignore ? 0 : t >= 0 && t < a.V ? 1 : -1;
+    if (state == 1) loss = kLn2 * (lse - a.pick[row]);
+  }
+  if (state == 0) {
+    lse = __builtin_inff();
+    loss = 0.f;
+  } else if (state < 0) {
+    lse = loss = __builtin_nanf("");
+  }
+  if (lane == 0) {
+    a.lse2[row] = lse;
+    a.row_loss[row] = loss;
+  }
+}
+
+// One workgroup: thread t adds rows t, t + 1024, ... in order, then a tree.
+__global__ __launch_bounds__(1024) void mean_loss_kernel(const RowLossArgs a) {
+  __shared__ float sums[1024];
+  __shared__ int counts[1024];
+  const int t = threadIdx.x;
+  float s = 0.f;
+  int n = 0;
+  for (int64_t r = t; r < a.M; r += 1024) {
+    s += a.row_loss[r];
+    n += a.lse2[r] != __builtin_inff();
+  }
+  sums[t] = s;
+  counts[t] = n;
+  __syncthreads();
+  for (int h = 512; h > 0; h >>= 1) {
+    if (t < h) {
+      sums[t] += sums[t + h];
+      counts[t] += counts[t + h];
+    }
+    __syncthreads();
+  }
+  if (t == 0) {
+    const float inv = 1.f / (float)(counts[0] > 0 ? counts[0] : 1);
+    if (a.loss) *a.loss = sums[0] * inv;
+    *a.alpha = a.temperature * inv;
+  }
+}
+
+hipError_t launch_row_loss(const RowLossArgs& a, hipStream_t s) {
+  if (a.M > 0) {
+    hipLaunchKernelGGL(row_loss_kernel, dim3((unsigned)cdiv(a.M, 4)), dim3(256), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(mean_loss_kernel, dim3(1), dim3(1024), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace ffmlp
