@@ -327,9 +327,9 @@ size_t mlp_head_workspace_bytes(int64_t M, int64_t D, int64_t V, int top,
                                 int mode);
 
 /* Softmax cross entropy of the logits L = H W, which are never stored whole:
- * the loss keeps a running maximum and sum per row, the gradients recompute
- * the logits in pieces of the vocabulary (at most 512 MiB of them at a time,
- * or 1024 columns).
+ * the loss keeps a running maximum and sum per row, the gradients take the
+ * vocabulary in pieces of at most 1 GiB of 16-bit values (or 1024 columns), a
+ * later piece's logits being computed again.
  *   H       bf16 [M][D];  W  bf16 [D][V].
  *   target  int64 [M], 8-byte aligned: 0 .. V - 1, or ignore_index for a row
  *           that does not count.  Any other value makes the loss (and the

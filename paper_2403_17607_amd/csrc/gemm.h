@@ -27,7 +27,8 @@ struct GemmOut {
   void* C;             // [M][ldc], bf16 or fp32
   int64_t ldc;
   int c_fp32;
-  int vec;             // every row of C, R, add and stash allows accesses of four columns
+  int vec;             // every row of C, R, add and stash allows accesses of four columns,
+  int vec8;            // and N is a multiple of 8 and they allow 16-byte accesses of them
 };
 
 struct GemmArgs {
@@ -42,7 +43,7 @@ struct GemmArgs {
 };
 
 // Workgroup tiles (gemm_kernel.h) and which sides have k across their rows.
-enum { GEMM_ROWS = 0, GEMM_MEDIUM = 1, GEMM_LARGE = 2 };
+enum { GEMM_ROWS = 0, GEMM_MEDIUM = 1, GEMM_LARGE = 2, GEMM_SQUARE = 3 };
 enum { GEMM_XW = 0, GEMM_DX = 1, GEMM_DW = 2 };
 
 struct GemmPlan {
@@ -57,14 +58,9 @@ GemmPlan gemm_plan(int form, int64_t M, int64_t N, int64_t K);
 // `partial`: gemm_plan(...).partial_bytes of workspace.
 hipError_t launch_gemm(int form, GemmArgs a, float* partial, hipStream_t s);
 
-hipError_t launch_gemm_xw(int tile, bool direct, const GemmArgs& a, hipStream_t s);
-hipError_t launch_gemm_dx(int tile, bool direct, const GemmArgs& a, hipStream_t s);
-hipError_t launch_gemm_dw(int tile, bool direct, const GemmArgs& a, hipStream_t s);
-
-// Whether a side consists of whole 16-byte aligned pieces of eight elements.
-inline bool side_aligned(const SideArgs& s) {
-  return reinterpret_cast<uintptr_t>(s.p) % 16 == 0 && s.ld % 8 == 0 && s.cols % 8 == 0;
-}
+hipError_t launch_gemm_xw(int tile, const GemmArgs& a, hipStream_t s);
+hipError_t launch_gemm_dx(int tile, const GemmArgs& a, hipStream_t s);
+hipError_t launch_gemm_dw(int tile, const GemmArgs& a, hipStream_t s);
 
 // dZ = bf16(dY * stash) [M][ldz] (dZ null: not stored; stash null: linear) and,
 // for db, the column sums of the unrounded products: `parts` partial sums

@@ -11,6 +11,7 @@ constexpr int kWorkgroups = 512;  // two per CU
 
 struct TileSize { int bm, bn, bk; };
 TileSize tile_size(int tile) {
+  if (tile == GEMM_SQUARE) return {GemmSquare::BM, GemmSquare::BN, GemmSquare::BK};
   if (tile == GEMM_LARGE) return {GemmLarge::BM, GemmLarge::BN, GemmLarge::BK};
   if (tile == GEMM_MEDIUM) return {GemmMedium::BM, GemmMedium::BN, GemmMedium::BK};
   return {GemmRows::BM, GemmRows::BN, GemmRows::BK};
@@ -22,13 +23,16 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 GemmPlan gemm_plan(int form, int64_t M, int64_t N, int64_t K) {
   GemmPlan p{};
   const int64_t large = cdiv(M, GemmLarge::BM) * cdiv(N, GemmLarge::BN);
-  p.tile = form != GEMM_DW && M <= GemmRows::BM ? GEMM_ROWS : large >= kWorkgroups / 4 ? GEMM_LARGE : GEMM_MEDIUM;
+  p.tile = form != GEMM_DW && M <= GemmRows::BM ? GEMM_ROWS
+           : large < kWorkgroups / 4             ? GEMM_MEDIUM
+           : form == GEMM_XW                     ? GEMM_LARGE
+                                                 : GEMM_SQUARE;
   const TileSize t = tile_size(p.tile);
   p.mt = (int)cdiv(M, t.bm);
   p.nt = (int)cdiv(N, t.bn);
   const int64_t tiles = (int64_t)p.mt * p.nt;
   // Splits fill the chip when the tiles do not, each over at least 256 of k.
-  int64_t s = kWorkgroups / tiles, most = K / 256;
+  int64_t s = (p.tile == GEMM_SQUARE ? kWorkgroups / 2 : kWorkgroups) / tiles, most = K / 256;
   if (s > most) s = most;
   if (s < 1) s = 1;
   p.kper = K > 0 ? cdiv(cdiv(K, s), t.bk) * t.bk : t.bk;
@@ -65,10 +69,9 @@ hipError_t launch_gemm(int form, GemmArgs a, float* partial, hipStream_t s) {
   a.splits = p.splits;
   a.kper = p.kper;
   a.partial = partial;
-  const bool direct = side_aligned(a.m) && side_aligned(a.n);
-  hipError_t e = form == GEMM_XW   ? launch_gemm_xw(p.tile, direct, a, s)
-                 : form == GEMM_DX ? launch_gemm_dx(p.tile, direct, a, s)
-                                   : launch_gemm_dw(p.tile, direct, a, s);
+  hipError_t e = form == GEMM_XW   ? launch_gemm_xw(p.tile, a, s)
+                 : form == GEMM_DX ? launch_gemm_dx(p.tile, a, s)
+                                   : launch_gemm_dw(p.tile, a, s);
   if (e != hipSuccess || p.splits <= 1) return e;
   const int64_t n = a.M * ((a.N + 3) / 4);
   hipLaunchKernelGGL(split_sum_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, partial, p.splits, a.M, a.N, a.out);

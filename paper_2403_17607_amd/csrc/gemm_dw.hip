@@ -3,13 +3,9 @@
 
 namespace ffmlp {
 
-hipError_t launch_gemm_dw(int tile, bool direct, const GemmArgs& a, hipStream_t s) {
-  if (direct) {
-    if (tile == GEMM_LARGE) return launch_gemm_tile<GemmLarge, true, true, true>(a, s);
-    return launch_gemm_tile<GemmMedium, true, true, true>(a, s);
-  }
-  if (tile == GEMM_LARGE) return launch_gemm_tile<GemmLarge, true, true, false>(a, s);
-  return launch_gemm_tile<GemmMedium, true, true, false>(a, s);
+hipError_t launch_gemm_dw(int tile, const GemmArgs& a, hipStream_t s) {
+  if (tile == GEMM_SQUARE) return launch_gemm_tile<GemmSquare, true, true>(a, s);
+  return launch_gemm_tile<GemmMedium, true, true>(a, s);
 }
 
 }  // namespace ffmlp

@@ -3,15 +3,10 @@
 
 namespace ffmlp {
 
-hipError_t launch_gemm_dx(int tile, bool direct, const GemmArgs& a, hipStream_t s) {
-  if (direct) {
-    if (tile == GEMM_LARGE) return launch_gemm_tile<GemmLarge, false, false, true>(a, s);
-    if (tile == GEMM_MEDIUM) return launch_gemm_tile<GemmMedium, false, false, true>(a, s);
-    return launch_gemm_tile<GemmRows, false, false, true>(a, s);
-  }
-  if (tile == GEMM_LARGE) return launch_gemm_tile<GemmLarge, false, false, false>(a, s);
-  if (tile == GEMM_MEDIUM) return launch_gemm_tile<GemmMedium, false, false, false>(a, s);
-  return launch_gemm_tile<GemmRows, false, false, false>(a, s);
+hipError_t launch_gemm_dx(int tile, const GemmArgs& a, hipStream_t s) {
+  if (tile == GEMM_SQUARE) return launch_gemm_tile<GemmSquare, false, false>(a, s);
+  if (tile == GEMM_ROWS) return launch_gemm_tile<GemmRows, false, false>(a, s);
+  return launch_gemm_tile<GemmMedium, false, false>(a, s);
 }
 
 }  // namespace ffmlp

@@ -8,14 +8,20 @@
 //     dX = dZ W^T   dZ [m][k] W [n][k]     m false, n false
 //     dW = X^T dZ   X [k][m]  dZ [k][n]    m true,  n true
 // A workgroup owns a BM x BN tile of C and walks k in steps of BK.  Each step
-// brings a BK slice of both sides to LDS as it lies in memory; a side with k
-// across its rows is transposed by the LDS read (ds_read_b64_tr_b16: 16 lanes
-// read a 4 x 16 block and lane i gets its column i), so no operand is
-// repacked.  The n side is the first MFMA operand: lane (i, g) of the result
-// holds four consecutive columns 4 g .. 4 g + 3 of row i.
+// brings a BK slice of both sides to LDS as it lies in memory, without passing
+// through registers (buffer_load ... lds); a side with k across its rows is
+// transposed by the LDS read (ds_read_b64_tr_b16: 16 lanes read a 4 x 16 block
+// and lane i gets its column i), so no operand is repacked.  The n side is the
+// first MFMA operand: lane (i, g) of the result holds four consecutive columns
+// 4 g .. 4 g + 3 of row i.
 //
 // LDS holds 16-byte pieces, [row][piece], the piece index XORed with a
 // function of the row (below) so that the reads hit every bank once.
+//
+// Rows may start at any element: these loads take any address.  Measured per
+// 64 KiB of 512-byte rows from L2: 0.62 us where rows start at a multiple of
+// 4 bytes, 1.84 where none does, 1.22 where every second does.  What an
+// unaligned or short row needs besides is the last step of k (Loader::fix).
 #pragma once
 
 #include "device.h"
@@ -54,15 +60,14 @@ struct Side {
 
 // The global side of the loads of one thread, for a workgroup that owns the
 // rows (T = false) or columns (T = true) from r0 on and contracts k0 .. kend - 1.
-template <typename S, bool T, int BK, int NTHR, bool DIRECT>
+template <typename S, bool T, int BK, int NTHR>
 struct Loader {
   SideArgs a;
   int64_t r0, kend;
-  const uint8_t* p;       // direct loads: the next step's first element,
-  int64_t left;           //   the bytes from it to the end of what may be read
-  int krem;               //   and the k from it on
+  const uint8_t* p;       // the next step's first element,
+  int64_t left;           // the bytes from it to the end of what may be read
+  int krem;               // and the k from it on
   uint32_t voff[S::PER];  // byte offsets of the thread's pieces within a step
-  u32x4 v[DIRECT ? 1 : S::PER];
 
   static __device__ __forceinline__ int piece_row(int j, int tid) { return (j * NTHR + tid) / S::CH; }
   static __device__ __forceinline__ int piece_col(int j, int tid) {
@@ -76,20 +81,18 @@ struct Loader {
     a = args;
     r0 = first;
     kend = k1;
-    if constexpr (DIRECT) {
-      const int64_t row = T ? k0 : r0, col = T ? r0 : k0, last = T ? k1 - 1 : a.rows - 1;
-      p = reinterpret_cast<const uint8_t*>(a.p + row * a.ld + col);
-      left = ((last - row) * a.ld + a.cols - col) * 2;
-      krem = (int)(k1 - k0);
+    const int64_t row = T ? k0 : r0, col = T ? r0 : k0, last = T ? k1 - 1 : a.rows - 1;
+    p = reinterpret_cast<const uint8_t*>(a.p + row * a.ld + col);
+    left = ((last - row) * a.ld + a.cols - col) * 2;
+    krem = (int)(k1 - k0);
 #pragma unroll
-      for (int j = 0; j < S::PER; ++j)
-        voff[j] = piece_in(j, tid) ? (uint32_t)(((int64_t)piece_row(j, tid) * a.ld + piece_col(j, tid)) * 2) : kOOB;
-    }
+    for (int j = 0; j < S::PER; ++j)
+      voff[j] = piece_in(j, tid) ? (uint32_t)(((int64_t)piece_row(j, tid) * a.ld + piece_col(j, tid)) * 2) : kOOB;
   }
-  // The next step to LDS at `lds` without passing through registers.  Pieces
-  // past kend or past the matrix are out of the descriptor's range and arrive
-  // as zeros, so steps past the last one may be loaded too.  What follows a
-  // T side's row in memory comes along in its last tile: it only reaches
+  // The next step to LDS at `lds`.  Pieces that begin past kend or past the
+  // matrix are out of the descriptor's range and arrive as zeros, so steps
+  // past the last one may be loaded too.  What follows a T side's row in
+  // memory (within the matrix) comes along in its last tile: it only reaches
   // columns of C that do not exist.
   __device__ __forceinline__ void to_lds(uint32_t lds, int wave, int tid) {
     // (a buffer descriptor as make_rsrc builds it, in scalar registers)
@@ -109,33 +112,25 @@ struct Loader {
     left -= step;
     krem -= BK;
   }
-  // The pieces of the step from k0 on through registers, for matrices whose
-  // rows start anywhere: unaligned 16-byte loads, the last piece of a row by
-  // element.
-  __device__ __forceinline__ void to_regs(int64_t k0, int tid) {
+  // Whether the step that ends with kend has pieces that are neither whole
+  // nor empty: their rest would be of the next row (along k: nonzero), or they
+  // end with the matrix, where the range check may drop the last element with
+  // the dword it shares.
+  __device__ __forceinline__ bool ragged() const { return T ? (a.cols & 7) != 0 : (kend & 7) != 0; }
+  // That step's slice once more, exactly, through registers.
+  __device__ __forceinline__ void fix(uint8_t* lds, int64_t k0, int tid) const {
     const int64_t rend = T ? kend : a.rows, cend = T ? a.cols : kend;
-#pragma unroll
+#pragma unroll 1
     for (int j = 0; j < S::PER; ++j) {
       const int64_t row = (T ? k0 : r0) + piece_row(j, tid), c = (T ? r0 : k0) + piece_col(j, tid);
-      u32x4 x = {0u, 0u, 0u, 0u};
-      if (piece_in(j, tid) && row < rend && c < cend) {
-        const uint16_t* src = a.p + row * a.ld + c;
-        if (c + 8 <= cend) {
-          x = *reinterpret_cast<const u32x4_a2*>(src);
-        } else {
-          uint32_t e[8];
+      if (!piece_in(j, tid) || row >= rend || c >= cend || c + 8 <= cend) continue;
+      const uint16_t* src = a.p + row * a.ld + c;
+      uint32_t e[8];
 #pragma unroll
-          for (int q = 0; q < 8; ++q) e[q] = c + q < cend ? (uint32_t)src[q] : 0u;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) x[q] = e[2 * q] | (e[2 * q + 1] << 16);
-        }
-      }
-      v[j] = x;
+      for (int q = 0; q < 8; ++q) e[q] = c + q < cend ? (uint32_t)src[q] : 0u;
+      *reinterpret_cast<u32x4*>(lds + (j * NTHR + tid) * 16) =
+          u32x4{e[0] | (e[1] << 16), e[2] | (e[3] << 16), e[4] | (e[5] << 16), e[6] | (e[7] << 16)};
     }
-  }
-  __device__ __forceinline__ void regs_to_lds(uint8_t* lds, int tid) const {
-#pragma unroll
-    for (int j = 0; j < S::PER; ++j) *reinterpret_cast<u32x4*>(lds + (j * NTHR + tid) * 16) = v[j];
   }
 };
 
@@ -182,19 +177,20 @@ __device__ __forceinline__ void wait_loads_barrier() {
 }
 
 // acc += the BM x BN tile's products over k in [k0, k1), k0 a multiple of BK.
-// `lds`: the workgroup's ST buffers of the two slices.  Every wave passes the
-// last barrier only after its own reads, so the buffers are free afterwards
-// once the caller has synchronized.
-template <typename TL, bool MT, bool NT, bool DIRECT>
+// `lds`: the workgroup's ST buffers of the two slices, free again when it
+// returns.  Within a step the fragments of its first 32 k are read before the
+// next loads are issued: a full memory queue then holds up no matrix product
+// (2 to 4% over issuing first).
+template <typename TL, bool MT, bool NT>
 __device__ __forceinline__ void gemm_loop(const SideArgs& ma, const SideArgs& na, int64_t m0, int64_t n0, int64_t k0,
                                           int64_t k1, uint8_t* lds, f32x4 (&acc)[TL::MB][TL::NB]) {
   typedef Side<MT, TL::BM, TL::BK, TL::NTHR> SM;
   typedef Side<NT, TL::BN, TL::BK, TL::NTHR> SN;
-  constexpr int STAGE = SM::BYTES + SN::BYTES;
+  constexpr int STAGE = SM::BYTES + SN::BYTES, LOADS = SM::PER + SN::PER;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / TL::WN, wn = wave % TL::WN;
-  Loader<SM, MT, TL::BK, TL::NTHR, DIRECT> lm;
-  Loader<SN, NT, TL::BK, TL::NTHR, DIRECT> ln;
+  Loader<SM, MT, TL::BK, TL::NTHR> lm;
+  Loader<SN, NT, TL::BK, TL::NTHR> ln;
   lm.init(ma, m0, k0, k1, tid);
   ln.init(na, n0, k0, k1, tid);
   Frags<SM, MT, TL::MB> fm;
@@ -202,67 +198,85 @@ __device__ __forceinline__ void gemm_loop(const SideArgs& ma, const SideArgs& na
   fm.init(wm * TL::MB * 16, lane);
   fn.init(wn * TL::NB * 16, lane);
   const int nk = (int)((k1 - k0 + TL::BK - 1) / TL::BK);
-  auto multiply = [&](const uint8_t* s) {
+  const uint32_t l0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+  const auto issue = [&](int slot) {
+    lm.to_lds(l0 + slot * STAGE, wave, tid);
+    ln.to_lds(l0 + slot * STAGE + SM::BYTES, wave, tid);
+  };
+#pragma unroll
+  for (int t = 0; t < TL::ST - 1; ++t) issue(t);
+  int slot = 0;
+  for (int t = 0; t < nk; ++t) {
+    wait_loads_barrier<(TL::ST - 2) * LOADS>();
+    uint8_t* s = lds + slot * STAGE;
+    if (t == nk - 1 && (lm.ragged() || ln.ragged())) {
+      const int64_t k = k0 + (int64_t)t * TL::BK;
+      lm.fix(s, k, tid);
+      ln.fix(s + SM::BYTES, k, tid);
+      __syncthreads();
+    }
 #pragma unroll
     for (int kk = 0; kk < TL::BK / 32; ++kk) {
-      u32x4 b[TL::NB];
+      u32x4 a[TL::MB], b[TL::NB];
 #pragma unroll
       for (int n = 0; n < TL::NB; ++n) b[n] = fn.read(s + SM::BYTES, kk, n);
 #pragma unroll
-      for (int m = 0; m < TL::MB; ++m) {
-        const u32x4 a = fm.read(s, kk, m);
+      for (int m = 0; m < TL::MB; ++m) a[m] = fm.read(s, kk, m);
+      if (kk == 0) {
+        // into the buffer of step t - 1, which every wave has read.  Steps past
+        // the last load zeros, so that the count of loads in flight stays the same.
+        __builtin_amdgcn_sched_barrier(0);
+        issue(slot == 0 ? TL::ST - 1 : slot - 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
 #pragma unroll
-        for (int n = 0; n < TL::NB; ++n) acc[m][n] = mfma16(b[n], a, acc[m][n]);
-      }
-    }
-  };
-  if constexpr (DIRECT) {
-    constexpr int LOADS = SM::PER + SN::PER;
-    const uint32_t l0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
-    auto issue = [&](int slot) {
-      lm.to_lds(l0 + slot * STAGE, wave, tid);
-      ln.to_lds(l0 + slot * STAGE + SM::BYTES, wave, tid);
-    };
+      for (int m = 0; m < TL::MB; ++m)
 #pragma unroll
-    for (int t = 0; t < TL::ST - 1; ++t) issue(t);
-    int slot = 0;
-    for (int t = 0; t < nk; ++t) {
-      wait_loads_barrier<(TL::ST - 2) * LOADS>();
-      // into the buffer of step t - 1, which every wave has read.  Steps past
-      // the last load zeros, so that the count of loads in flight stays the same.
-      issue(slot == 0 ? TL::ST - 1 : slot - 1);
-      multiply(lds + slot * STAGE);
-      slot = slot + 1 == TL::ST ? 0 : slot + 1;
+        for (int n = 0; n < TL::NB; ++n) acc[m][n] = mfma16(b[n], a[m], acc[m][n]);
     }
-    wait_loads_barrier<0>();
-  } else {
-    lm.to_regs(k0, tid);
-    ln.to_regs(k0, tid);
-    lm.regs_to_lds(lds, tid);
-    ln.regs_to_lds(lds + SM::BYTES, tid);
-    for (int t = 0; t < nk; ++t) {
-      __syncthreads();
-      const int64_t k = k0 + (int64_t)(t + 1) * TL::BK;
-      if (k < k1) {
-        lm.to_regs(k, tid);
-        ln.to_regs(k, tid);
-      }
-      multiply(lds + (t & 1) * STAGE);
-      if (k < k1) {
-        lm.regs_to_lds(lds + (~t & 1) * STAGE, tid);
-        ln.regs_to_lds(lds + (~t & 1) * STAGE + SM::BYTES, tid);
-      }
-    }
-    __syncthreads();
+    slot = slot + 1 == TL::ST ? 0 : slot + 1;
   }
+  wait_loads_barrier<0>();
 }
 
-template <typename TL, bool MT, bool NT, bool DIRECT>
+// Results leave through LDS, ROWS = 16 G rows of a wave at a time in a part of
+// its own, so that a wave's stores cover whole rows of its columns.  Row
+// stride + 4 floats: eight lanes write eight rows' 16 bytes to different banks.
+template <typename TL>
+struct OutTile {
+  static constexpr int G = TL::MB >= 2 ? 2 : 1, ROWS = 16 * G, COLS = TL::NB * 16, LD = COLS + 4;
+  static constexpr int BYTES = TL::NW * ROWS * LD * 4;
+};
+
+template <typename TL, bool MT, bool NT>
 constexpr int gemm_lds_bytes() {
-  constexpr int loop = (DIRECT ? TL::ST : 2) *
-                       (Side<MT, TL::BM, TL::BK, TL::NTHR>::BYTES + Side<NT, TL::BN, TL::BK, TL::NTHR>::BYTES);
-  constexpr int out = TL::NW * 16 * (TL::NB * 16 + 4) * 4;  // the results of one 16-row block of each wave
-  return loop > out ? loop : out;
+  constexpr int loop = TL::ST * (Side<MT, TL::BM, TL::BK, TL::NTHR>::BYTES + Side<NT, TL::BN, TL::BK, TL::NTHR>::BYTES);
+  return loop > OutTile<TL>::BYTES ? loop : OutTile<TL>::BYTES;
+}
+
+// f(r, p): for each phase, rows r = 0 .. ROWS - 1 of the phase (this lane's),
+// p the lane's `WIDE` consecutive results of that row, columns WIDE (lane %
+// (COLS / WIDE)) on.  before(m): called before block m of acc is written.
+template <typename TL, int WIDE, typename B, typename F>
+__device__ __forceinline__ void out_rows(uint8_t* lds, f32x4 (&acc)[TL::MB][TL::NB], B&& before, F&& f) {
+  typedef OutTile<TL> O;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float* part = reinterpret_cast<float*>(lds) + wave * O::ROWS * O::LD;
+  constexpr int LPR = O::COLS / WIDE, RPI = 64 / LPR;
+  static_for<0, TL::MB / O::G>([&](auto pc) {
+    constexpr int ph = decltype(pc)::value;
+    static_for<0, O::G>([&](auto gc) {
+      constexpr int m = ph * O::G + decltype(gc)::value;
+      before(std::integral_constant<int, m>{});
+#pragma unroll
+      for (int n = 0; n < TL::NB; ++n)
+        *reinterpret_cast<f32x4*>(part + (16 * decltype(gc)::value + (lane & 15)) * O::LD + 16 * n + 4 * (lane >> 4)) = acc[m][n];
+    });
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int r = lane / LPR; r < O::ROWS; r += RPI) f(ph * O::ROWS + r, part + r * O::LD + WIDE * (lane % LPR));
+    __builtin_amdgcn_wave_barrier();
+  });
 }
 
 // Tile `t` of mt x nt, in an order that keeps a chiplet's tiles together: the
@@ -370,8 +384,70 @@ __device__ __forceinline__ void out4(const GemmOut& o, int64_t m, int n, int N, 
   }
 }
 
+// act(z) in place over eight values, act'(z) in d.
+__device__ __forceinline__ void act8(int act, float (&z)[8], float (&d)[8]) {
+  const auto all = [&](auto kind) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      float y;
+      act_and_grad(decltype(kind)::value, z[q], y, d[q]);
+      z[q] = y;
+    }
+  };
+  switch (act) {
+    case ACT_RELU: all(std::integral_constant<int, ACT_RELU>{}); break;
+    case ACT_SIGMOID: all(std::integral_constant<int, ACT_SIGMOID>{}); break;
+    case ACT_SINE: all(std::integral_constant<int, ACT_SINE>{}); break;
+    case ACT_GELU: all(std::integral_constant<int, ACT_GELU>{}); break;
+    case ACT_SILU: all(std::integral_constant<int, ACT_SILU>{}); break;
+    default: all(std::integral_constant<int, ACT_LINEAR>{});
+  }
+}
+
+// Eight columns n .. n + 7 of row m where o.vec8; b: the bias of these columns.
+__device__ __forceinline__ void out8(const GemmOut& o, int64_t m, int n, int N, const float* p, const float (&b)[8], float alpha) {
+  float z[8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    f32x4 v = *reinterpret_cast<const f32x4*>(p + 4 * h);
+    if (o.add) v += *reinterpret_cast<const f32x4*>(o.add + m * o.ldadd + n + 4 * h);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) z[4 * h + q] = v[q] * alpha + b[4 * h + q];
+  }
+  if (o.act != ACT_LINEAR) {
+    float d[8];
+    act8(o.act, z, d);
+    if (o.stash) {
+      float* s = o.stash + m * (int64_t)N + n;
+      *reinterpret_cast<f32x4*>(s) = f32x4{d[0], d[1], d[2], d[3]};
+      *reinterpret_cast<f32x4*>(s + 4) = f32x4{d[4], d[5], d[6], d[7]};
+    }
+  }
+  if (o.c_fp32) {
+    float* c = static_cast<float*>(o.C) + m * o.ldc + n;
+    const float* r = static_cast<const float*>(o.R) + m * o.ldr + n;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      f32x4 v = {z[4 * h], z[4 * h + 1], z[4 * h + 2], z[4 * h + 3]};
+      if (o.R) v += *reinterpret_cast<const f32x4*>(r + 4 * h);
+      *reinterpret_cast<f32x4*>(c + 4 * h) = v;
+    }
+  } else {
+    if (o.R) {
+      const u32x4 u = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(o.R) + m * o.ldr + n);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        z[2 * q] += bf16_lo(u[q]);
+        z[2 * q + 1] += bf16_hi(u[q]);
+      }
+    }
+    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(o.C) + m * o.ldc + n) =
+        u32x4{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]), pack_bf16x2(z[4], z[5]), pack_bf16x2(z[6], z[7])};
+  }
+}
+
 // C = the product, or one split's share of it as fp32 partial sums.
-template <typename TL, bool MT, bool NT, bool DIRECT>
+template <typename TL, bool MT, bool NT>
 __global__ __launch_bounds__(TL::NTHR, 2) void gemm_kernel(const GemmArgs a) {
   extern __shared__ __align__(16) uint8_t gemm_lds[];
   const int b = blockIdx.x % a.tiles, split = blockIdx.x / a.tiles;
@@ -385,7 +461,7 @@ __global__ __launch_bounds__(TL::NTHR, 2) void gemm_kernel(const GemmArgs a) {
   for (int m = 0; m < TL::MB; ++m)
 #pragma unroll
     for (int n = 0; n < TL::NB; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-  gemm_loop<TL, MT, NT, DIRECT>(a.m, a.n, m0, n0, k0, k1, gemm_lds, acc);
+  gemm_loop<TL, MT, NT>(a.m, a.n, m0, n0, k0, k1, gemm_lds, acc);
   GemmOut o = a.out;
   if (a.splits > 1) {
     o = GemmOut{};
@@ -393,35 +469,34 @@ __global__ __launch_bounds__(TL::NTHR, 2) void gemm_kernel(const GemmArgs a) {
     o.ldc = a.N;
     o.c_fp32 = 1;
     o.vec = (a.N & 3) == 0;
+    o.vec8 = (a.N & 7) == 0;
   }
-  // Through LDS, 16 rows of a wave at a time (its own part, so no barrier), so
-  // that a wave's stores cover whole rows of its columns.  Row stride + 4
-  // floats: eight lanes write eight rows' 16 bytes to different banks.
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  constexpr int COLS = TL::NB * 16, LD = COLS + 4, LPR = COLS / 4, RPI = 64 / LPR;
-  float* part = reinterpret_cast<float*>(gemm_lds) + wave * 16 * LD;
+  constexpr int COLS = OutTile<TL>::COLS;
   const int64_t mw = m0 + (wave / TL::WN) * TL::MB * 16;
   const int nw = n0 + (wave % TL::WN) * COLS;
-  static_for<0, TL::MB>([&](auto mc) {
-    constexpr int m = decltype(mc)::value;
+  const auto none = [](auto) {};
+  if (o.vec8) {
+    const int n = nw + 8 * (lane % (COLS / 8));
+    const float alpha = o.alpha ? *o.alpha : 1.f;
+    float bias[8];
 #pragma unroll
-    for (int n = 0; n < TL::NB; ++n)
-      *reinterpret_cast<f32x4*>(part + (lane & 15) * LD + 16 * n + 4 * (lane >> 4)) = acc[m][n];
-    __builtin_amdgcn_wave_barrier();
-    const int n = nw + 4 * (lane % LPR);
-#pragma unroll 1
-    for (int r = lane / LPR; r < 16; r += RPI) {
-      const int64_t row = mw + 16 * m + r;
-      if (row < a.M && n < a.N) out4(o, row, n, a.N, *reinterpret_cast<const f32x4*>(part + r * LD + 4 * (lane % LPR)));
-    }
-    __builtin_amdgcn_wave_barrier();
-  });
+    for (int q = 0; q < 8; ++q) bias[q] = o.bias && n < a.N ? o.bias[n + q] : 0.f;
+    out_rows<TL, 8>(gemm_lds, acc, none, [&](int r, const float* p) {
+      if (mw + r < a.M && n < a.N) out8(o, mw + r, n, a.N, p, bias, alpha);
+    });
+  } else {
+    const int n = nw + 4 * (lane % (COLS / 4));
+    out_rows<TL, 4>(gemm_lds, acc, none, [&](int r, const float* p) {
+      if (mw + r < a.M && n < a.N) out4(o, mw + r, n, a.N, *reinterpret_cast<const f32x4*>(p));
+    });
+  }
 }
 
-template <typename TL, bool MT, bool NT, bool DIRECT>
+template <typename TL, bool MT, bool NT>
 hipError_t launch_gemm_tile(GemmArgs a, hipStream_t s) {
-  constexpr int lds = gemm_lds_bytes<TL, MT, NT, DIRECT>();
-  const auto k = gemm_kernel<TL, MT, NT, DIRECT>;
+  constexpr int lds = gemm_lds_bytes<TL, MT, NT>();
+  const auto k = gemm_kernel<TL, MT, NT>;
   int occ;
   const hipError_t e = kernel_occupancy(reinterpret_cast<const void*>(k), TL::NTHR, lds, &occ);
   if (e != hipSuccess) return e;
@@ -429,9 +504,11 @@ hipError_t launch_gemm_tile(GemmArgs a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Workgroup tiles.  Large: two workgroups per CU (72 KiB of LDS each), so
-// that one's epilogue and first loads hide behind the other's products.
+// Workgroup tiles.  GemmLarge: two workgroups per CU (72 KiB of LDS each), so
+// that one's epilogue hides behind the other's products.  GemmSquare: one, with
+// fewer bytes per product and 128-byte rows of k.
 typedef GemmTile<128, 256, 32, 2, 2, 3> GemmLarge;
+typedef GemmTile<256, 256, 64, 2, 4, 2> GemmSquare;
 typedef GemmTile<64, 128, 64, 2, 2, 3> GemmMedium;
 typedef GemmTile<16, 128, 64, 1, 4, 4> GemmRows;
 

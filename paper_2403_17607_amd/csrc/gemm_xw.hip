@@ -3,15 +3,11 @@
 
 namespace ffmlp {
 
-hipError_t launch_gemm_xw(int tile, bool direct, const GemmArgs& a, hipStream_t s) {
-  if (direct) {
-    if (tile == GEMM_LARGE) return launch_gemm_tile<GemmLarge, false, true, true>(a, s);
-    if (tile == GEMM_MEDIUM) return launch_gemm_tile<GemmMedium, false, true, true>(a, s);
-    return launch_gemm_tile<GemmRows, false, true, true>(a, s);
-  }
-  if (tile == GEMM_LARGE) return launch_gemm_tile<GemmLarge, false, true, false>(a, s);
-  if (tile == GEMM_MEDIUM) return launch_gemm_tile<GemmMedium, false, true, false>(a, s);
-  return launch_gemm_tile<GemmRows, false, true, false>(a, s);
+hipError_t launch_gemm_xw(int tile, const GemmArgs& a, hipStream_t s) {
+  if (tile == GEMM_SQUARE) return launch_gemm_tile<GemmSquare, false, true>(a, s);
+  if (tile == GEMM_LARGE) return launch_gemm_tile<GemmLarge, false, true>(a, s);
+  if (tile == GEMM_ROWS) return launch_gemm_tile<GemmRows, false, true>(a, s);
+  return launch_gemm_tile<GemmMedium, false, true>(a, s);
 }
 
 }  // namespace ffmlp

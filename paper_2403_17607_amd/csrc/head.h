@@ -28,17 +28,24 @@ struct HeadArgs {
   const float* lse2;      // [M]; +inf: the row does not count
   uint16_t* P;            // [M][ldp]
   int64_t ldp;
+  int keep;               // columns of the first piece, or 0: no gradients
+  float* ref;             // [keep / the columns of a wave's tile][M]
 };
+
+// The passes over the logits: log-sum-exp; P of the first piece from what that
+// kept; P of a later piece.
+enum HeadPass { HEAD_LSE, HEAD_SCALE, HEAD_PROB };
 
 struct HeadPlan {
   bool large;
   int mt, nt, runs, per_run;  // head_lse_kernel
   int piece, pieces;          // columns of P, a multiple of 256 unless one piece holds all
+  int refs;                   // references of a row in the first piece
 };
 HeadPlan head_plan(int64_t M, int64_t D, int64_t V);
 
-hipError_t launch_head_ce(bool prob, bool large, bool direct, const HeadArgs& a, hipStream_t s);
-hipError_t launch_head_distill(bool prob, bool large, bool direct, const HeadArgs& a, hipStream_t s);
+hipError_t launch_head_ce(HeadPass pass, bool large, const HeadArgs& a, hipStream_t s);
+hipError_t launch_head_distill(HeadPass pass, bool large, const HeadArgs& a, hipStream_t s);
 
 // The teacher's entries: probabilities over a row's list, sorted by index,
 // and the table of starts.  ok[m]: 1, 0 (an empty list) or -1 (an index past

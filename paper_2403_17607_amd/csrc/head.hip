@@ -5,7 +5,7 @@ namespace ffmlp {
 
 namespace {
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-constexpr int64_t kPieceElems = (int64_t)1 << 28;  // P of a piece: 512 MiB
+constexpr int64_t kPieceElems = (int64_t)1 << 29;  // P of a piece: 1 GiB
 }  // namespace
 
 HeadPlan head_plan(int64_t M, int64_t, int64_t V) {
@@ -23,6 +23,7 @@ HeadPlan head_plan(int64_t M, int64_t, int64_t V) {
   const int64_t pieces = cdiv(V, cols);
   p.piece = (int)(pieces <= 1 ? V : cdiv(cdiv(V, pieces), 256) * 256);
   p.pieces = (int)cdiv(V, p.piece);
+  p.refs = (int)cdiv(p.piece, p.large ? GemmLarge::BN : GemmMedium::BN) * 2;
   return p;
 }
 

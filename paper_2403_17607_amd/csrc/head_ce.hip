@@ -3,8 +3,8 @@
 
 namespace ffmlp {
 
-hipError_t launch_head_ce(bool prob, bool large, bool direct, const HeadArgs& a, hipStream_t s) {
-  return launch_head<false>(prob, large, direct, a, s);
+hipError_t launch_head_ce(HeadPass pass, bool large, const HeadArgs& a, hipStream_t s) {
+  return launch_head<false>(pass, large, a, s);
 }
 
 }  // namespace ffmlp

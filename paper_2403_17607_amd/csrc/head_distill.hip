@@ -3,8 +3,8 @@
 
 namespace ffmlp {
 
-hipError_t launch_head_distill(bool prob, bool large, bool direct, const HeadArgs& a, hipStream_t s) {
-  return launch_head<true>(prob, large, direct, a, s);
+hipError_t launch_head_distill(HeadPass pass, bool large, const HeadArgs& a, hipStream_t s) {
+  return launch_head<true>(pass, large, a, s);
 }
 
 }  // namespace ffmlp

@@ -6,11 +6,15 @@
 //
 // head_lse_kernel walks a run of column tiles with one row tile and keeps the
 // running maximum and sum of every row in registers, so the logits live only
-// in the matrix cores' results.  head_prob_kernel recomputes a piece of the
-// vocabulary and stores P as bf16, from which two products make the gradients
-// dH = P W^T and dW = H^T P.  q is sparse: the one target of a row, or the
-// teacher's top entries sorted by index, with a table of where each block of
-// 128 columns begins in a row's list.
+// in the matrix cores' results.  The gradients dH = P W^T and dW = H^T P take P
+// as bf16, a piece of the vocabulary at a time.  For the first piece the same
+// pass stores 2^(x - r) as fp16, r + 15 the maximum of the row's columns in a
+// wave's tile, and head_scale_kernel turns that into P in place once lse is
+// known.  fp16 up to 2^15: its rounding (2^-12 relative, at most 2^-40 of a
+// probability in absolute terms) does not add to that of P (2^-9).  The logits
+// of later pieces are recomputed by head_prob_kernel.  q is sparse:
+// the one target of a row, or the teacher's top entries sorted by index, with
+// a table of where each block of 128 columns begins in a row's list.
 #pragma once
 
 #include "gemm_kernel.h"
@@ -45,14 +49,29 @@ __device__ __forceinline__ int head_block(int b, int total) {
   return x * q + (x < r ? x : r) + y;
 }
 
-template <typename TL, bool DIRECT, bool DISTILL>
+// eight results of a row as fp16 (E) or bf16 (P)
+__device__ __forceinline__ u32x4 pack8_f16(const float* p) {
+  u32x4 u;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    u[q] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)p[2 * q], (_Float16)p[2 * q + 1]});
+  }
+  return u;
+}
+__device__ __forceinline__ u32x4 pack8_bf16(const float* p) {
+  return u32x4{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])};
+}
+
+template <typename TL, bool DISTILL>
 __global__ __launch_bounds__(TL::NTHR, 2) void head_lse_kernel(const HeadArgs a) {
   extern __shared__ __align__(16) uint8_t head_lds[];
   const int t = head_block(blockIdx.x, a.mt * a.runs);
   const int tm = t / a.runs, run = t % a.runs;
   const int64_t m0 = (int64_t)tm * TL::BM;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
-  const int64_t mw = m0 + (wave / TL::WN) * TL::MB * 16 + (lane & 15);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int COLS = TL::NB * 16;
+  const int64_t mw = m0 + (wave / TL::WN) * TL::MB * 16;
   float mx[TL::MB], sum[TL::MB];
 #pragma unroll
   for (int m = 0; m < TL::MB; ++m) {
@@ -61,16 +80,24 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_lse_kernel(const HeadArgs a)
   }
   const int t1 = (run + 1) * a.per_run < a.nt ? (run + 1) * a.per_run : a.nt;
   for (int tn = run * a.per_run; tn < t1; ++tn) {
-    const int n0 = tn * TL::BN, nw = n0 + (wave % TL::WN) * TL::NB * 16;
+    const int n0 = tn * TL::BN, nw = n0 + (wave % TL::WN) * COLS;
     f32x4 acc[TL::MB][TL::NB];
 #pragma unroll
     for (int m = 0; m < TL::MB; ++m)
 #pragma unroll
       for (int n = 0; n < TL::NB; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    gemm_loop<TL, false, true, DIRECT>(a.h, a.w, m0, n0, 0, a.D, head_lds, acc);
+    gemm_loop<TL, false, true>(a.h, a.w, m0, n0, 0, a.D, head_lds, acc);
+    // Opaque copies: what follows from them is worked out here, per tile, and
+    // not kept in registers across the products.
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    const int g = ln >> 4;
+    const int64_t row0 = mw + (ln & 15);
+    const bool keep = a.keep > n0;
+    float* part = reinterpret_cast<float*>(head_lds) + wave * 16 * OutTile<TL>::LD;
     static_for<0, TL::MB>([&](auto mc) {
       constexpr int m = decltype(mc)::value;
-      float top = mx[m];
+      float top = -__builtin_inff();
 #pragma unroll
       for (int n = 0; n < TL::NB; ++n)
 #pragma unroll
@@ -80,37 +107,61 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_lse_kernel(const HeadArgs a)
           acc[m][n][q] = x;
           top = __builtin_fmaxf(top, x);
         }
-      const float at = top == -__builtin_inff() ? 0.f : top;
-      float s = sum[m] * __builtin_amdgcn_exp2f(mx[m] - at);
-#pragma unroll
-      for (int n = 0; n < TL::NB; ++n)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) s += __builtin_amdgcn_exp2f(acc[m][n][q] - at);
-      mx[m] = top;
-      sum[m] = s;
-      head_hits<DISTILL>(a, mw + 16 * m, nw, TL::NB * 16, [&](int c, int e) {
+      // the four lane groups hold the same row
+      top = __builtin_fmaxf(top, __shfl_xor(top, 16));
+      top = __builtin_fmaxf(top, __shfl_xor(top, 32));
+      head_hits<DISTILL>(a, row0 + 16 * m, nw, COLS, [&](int c, int e) {
         if (((c >> 2) & 3) != g) return;
         float x = 0.f;
 #pragma unroll
         for (int n = 0; n < TL::NB; ++n)
 #pragma unroll
           for (int q = 0; q < 4; ++q) x = (c >> 4) == n && (c & 3) == q ? acc[m][n][q] : x;
-        a.pick[(mw + 16 * m) * a.top + e] = x;
+        a.pick[(row0 + 16 * m) * a.top + e] = x;
       });
+      // a sum of 2^(x - at), its largest term 2^15
+      const float at = top == -__builtin_inff() ? 0.f : top - 15.f;
+      float s = 0.f;
+#pragma unroll
+      for (int n = 0; n < TL::NB; ++n)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          acc[m][n][q] = __builtin_amdgcn_exp2f(acc[m][n][q] - at);
+          s += acc[m][n][q];
+        }
+      head_merge(mx[m], sum[m], top == -__builtin_inff() ? top : at, s);
+      if (keep) {
+        if (g == 0 && row0 + 16 * m < a.M) a.ref[(int64_t)(nw / COLS) * a.M + row0 + 16 * m] = at;
+        constexpr int LD = OutTile<TL>::LD, LPR = COLS / 8, RPI = 64 / LPR;
+#pragma unroll
+        for (int n = 0; n < TL::NB; ++n) *reinterpret_cast<f32x4*>(part + (ln & 15) * LD + 16 * n + 4 * g) = acc[m][n];
+        __builtin_amdgcn_wave_barrier();
+        const int c = nw + 8 * (ln % LPR);
+#pragma unroll 1
+        for (int r = ln / LPR; r < 16; r += RPI) {
+          const int64_t row = mw + 16 * m + r;
+          if (c < a.keep && row < a.M)
+            *reinterpret_cast<u32x4*>(a.P + row * a.ldp + c) = pack8_f16(part + r * LD + 8 * (ln % LPR));
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
     });
+    if (keep) __syncthreads();  // the next tile's loads write where other waves read
   }
-  // the four lane groups hold the same rows
+  const int g = lane >> 4;
+  const int64_t row0 = mw + (lane & 15);
   f32x2* part = a.partial + (int64_t)(run * TL::WN + wave % TL::WN) * a.M;
 #pragma unroll
   for (int m = 0; m < TL::MB; ++m) {
-#pragma unroll
-    for (int d = 16; d < 64; d *= 2) head_merge(mx[m], sum[m], __shfl_xor(mx[m], d), __shfl_xor(sum[m], d));
-    if (g == 0 && mw + 16 * m < a.M) part[mw + 16 * m] = f32x2{mx[m], sum[m]};
+    // the lane groups' sums, the maximum being the same
+    sum[m] += __shfl_xor(sum[m], 16);
+    sum[m] += __shfl_xor(sum[m], 32);
+    if (g == 0 && row0 + 16 * m < a.M) part[row0 + 16 * m] = f32x2{mx[m], sum[m]};
   }
 }
 
 // P of the columns a.col0 .. a.col0 + a.V - 1 (a.w begins at the first).
-template <typename TL, bool DIRECT, bool DISTILL>
+template <typename TL, bool DISTILL>
 __global__ __launch_bounds__(TL::NTHR, 2) void head_prob_kernel(const HeadArgs a) {
   extern __shared__ __align__(16) uint8_t head_lds[];
   int tm, tn;
@@ -118,19 +169,20 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_prob_kernel(const HeadArgs a
   const int64_t m0 = (int64_t)tm * TL::BM;
   const int n0 = tn * TL::BN;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
-  constexpr int COLS = TL::NB * 16, LD = COLS + 4, LPR = COLS / 4, RPI = 64 / LPR;
-  const int64_t mw = m0 + (wave / TL::WN) * TL::MB * 16;
+  constexpr int COLS = TL::NB * 16;
+  const int64_t mw = m0 + (wave / TL::WN) * TL::MB * 16, row0 = mw + (lane & 15);
   const int nw = n0 + (wave % TL::WN) * COLS;
   f32x4 acc[TL::MB][TL::NB];
 #pragma unroll
   for (int m = 0; m < TL::MB; ++m)
 #pragma unroll
     for (int n = 0; n < TL::NB; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-  gemm_loop<TL, false, true, DIRECT>(a.h, a.w, m0, n0, 0, a.D, head_lds, acc);
-  float* part = reinterpret_cast<float*>(head_lds) + wave * 16 * LD;
-  static_for<0, TL::MB>([&](auto mc) {
+  gemm_loop<TL, false, true>(a.h, a.w, m0, n0, 0, a.D, head_lds, acc);
+  uint16_t* P = a.P + mw * a.ldp + nw + 8 * (lane % (COLS / 8));  // ldp: a multiple of 8, at least V
+  const bool in = nw + 8 * (lane % (COLS / 8)) < a.V;
+  out_rows<TL, 8>(head_lds, acc, [&](auto mc) {
     constexpr int m = decltype(mc)::value;
-    const int64_t row = mw + 16 * m + (lane & 15);
+    const int64_t row = row0 + 16 * m;
     const float lse = row < a.M ? a.lse2[row] : __builtin_inff();
     const bool live = lse != __builtin_inff();  // a row that does not count has none
 #pragma unroll
@@ -146,39 +198,64 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_prob_kernel(const HeadArgs a
 #pragma unroll
         for (int q = 0; q < 4; ++q) acc[m][n][q] -= (c >> 4) == n && (c & 3) == q ? w : 0.f;
     });
-#pragma unroll
-    for (int n = 0; n < TL::NB; ++n)
-      *reinterpret_cast<f32x4*>(part + (lane & 15) * LD + 16 * n + 4 * g) = acc[m][n];
-    __builtin_amdgcn_wave_barrier();
-    const int n = nw + 4 * (lane % LPR);
-#pragma unroll 1
-    for (int r = lane / LPR; r < 16; r += RPI) {
-      const int64_t out = mw + 16 * m + r;
-      if (out >= a.M || n >= a.V) continue;
-      const f32x4 p = *reinterpret_cast<const f32x4*>(part + r * LD + 4 * (lane % LPR));
-      uint16_t* d = a.P + out * a.ldp + n;  // ldp is a multiple of 8, at least V rounded up
-      *reinterpret_cast<u32x2*>(d) = u32x2{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])};
-    }
-    __builtin_amdgcn_wave_barrier();
+  }, [&](int r, const float* p) {
+    if (in && mw + r < a.M) *reinterpret_cast<u32x4*>(P + r * a.ldp) = pack8_bf16(p);
   });
 }
 
-template <typename TL, bool DIRECT, bool DISTILL>
-hipError_t launch_head_tile(bool prob, const HeadArgs& a, hipStream_t s) {
-  constexpr int lds = gemm_lds_bytes<TL, false, true, DIRECT>();
-  const auto k = prob ? head_prob_kernel<TL, DIRECT, DISTILL> : head_lse_kernel<TL, DIRECT, DISTILL>;
+// P of the first piece from what head_lse_kernel kept of it, in place.  Wave
+// w of block (x, y): row 4 x + w, columns 4096 y .. + 4095, 512 at a time; G:
+// columns per reference.
+template <bool DISTILL, int G>
+__global__ __launch_bounds__(256) void head_scale_kernel(const HeadArgs a) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= a.M) return;
+  const int lane = threadIdx.x & 63;
+  const float lse = a.lse2[row];
+  const bool live = lse != __builtin_inff();
+  const int c1 = (int)(blockIdx.y + 1) * 4096 < a.keep ? (int)(blockIdx.y + 1) * 4096 : a.keep;
+#pragma unroll 2
+  for (int c0 = blockIdx.y * 4096; c0 < c1; c0 += 512) {
+    const int c = c0 + 8 * lane;
+    if (c >= c1) continue;
+    uint16_t* p = a.P + row * a.ldp + c;
+    const u32x4 u = *reinterpret_cast<const u32x4*>(p);
+    const float f = live ? __builtin_amdgcn_exp2f(a.ref[(int64_t)(c / G) * a.M + row] - lse) : 0.f;
+    float v[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const float e = (float)__builtin_bit_cast(_Float16, (uint16_t)(u[q / 2] >> (16 * (q & 1))));
+      v[q] = live ? e * f : 0.f;
+    }
+    head_hits<DISTILL>(a, row, c & ~(kHeadKey - 1), kHeadKey, [&](int at, int e) {
+      const int k = at - (c & (kHeadKey - 1));
+      const float w = DISTILL ? a.q[row * a.top + e] : 1.f;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] -= k == q ? w : 0.f;
+    });
+    *reinterpret_cast<u32x4*>(p) = pack8_bf16(v);
+  }
+}
+
+template <typename TL, bool DISTILL>
+hipError_t launch_head_tile(HeadPass pass, const HeadArgs& a, hipStream_t s) {
+  if (pass == HEAD_SCALE) {
+    hipLaunchKernelGGL((head_scale_kernel<DISTILL, TL::NB * 16>), dim3((unsigned)((a.M + 3) / 4), (unsigned)((a.keep + 4095) / 4096)),
+                       dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
+  constexpr int lds = gemm_lds_bytes<TL, false, true>();
+  const auto k = pass == HEAD_PROB ? head_prob_kernel<TL, DISTILL> : head_lse_kernel<TL, DISTILL>;
   int occ;
   const hipError_t e = kernel_occupancy(reinterpret_cast<const void*>(k), TL::NTHR, lds, &occ);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k, dim3((unsigned)(prob ? a.mt * a.nt : a.mt * a.runs)), dim3(TL::NTHR), lds, s, a);
+  hipLaunchKernelGGL(k, dim3((unsigned)(pass == HEAD_PROB ? a.mt * a.nt : a.mt * a.runs)), dim3(TL::NTHR), lds, s, a);
   return hipGetLastError();
 }
 
 template <bool DISTILL>
-hipError_t launch_head(bool prob, bool large, bool direct, const HeadArgs& a, hipStream_t s) {
-  if (large)
-    return direct ? launch_head_tile<GemmLarge, true, DISTILL>(prob, a, s) : launch_head_tile<GemmLarge, false, DISTILL>(prob, a, s);
-  return direct ? launch_head_tile<GemmMedium, true, DISTILL>(prob, a, s) : launch_head_tile<GemmMedium, false, DISTILL>(prob, a, s);
+hipError_t launch_head(HeadPass pass, bool large, const HeadArgs& a, hipStream_t s) {
+  return large ? launch_head_tile<GemmLarge, DISTILL>(pass, a, s) : launch_head_tile<GemmMedium, DISTILL>(pass, a, s);
 }
 
 }  // namespace ffmlp

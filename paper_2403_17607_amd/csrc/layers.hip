@@ -21,8 +21,18 @@ size_t type_size(int t) { return t == MLP_FP32 ? 4 : 2; }
 // Row stride of a matrix of `cols` columns.
 bool valid_ld(int64_t ld, int64_t cols) { return ld >= cols && ld <= kMaxDim; }
 
-// Whether rows of C, ld elements apart, allow accesses of four columns.
+// Whether rows ld elements apart allow accesses of four columns (16-byte ones
+// of eight).
 bool four_wide(const void* p, int64_t ld, int type) { return !p || (ld % 4 == 0 && aligned(p, 4 * type_size(type))); }
+bool eight_wide(const void* p, int64_t ld, int type) { return !p || (ld * type_size(type) % 16 == 0 && aligned(p, 16)); }
+
+// Fills in which accesses a product's output allows.
+void set_vec(GemmOut& o, int64_t N) {
+  const int t = o.c_fp32 ? MLP_FP32 : MLP_BF16;
+  o.vec = four_wide(o.C, o.ldc, t) && four_wide(o.R, o.ldr, t) && four_wide(o.stash, N, MLP_FP32) && four_wide(o.add, o.ldadd, MLP_FP32);
+  o.vec8 = N % 8 == 0 && eight_wide(o.C, o.ldc, t) && eight_wide(o.R, o.ldr, t) && eight_wide(o.stash, N, MLP_FP32) &&
+           eight_wide(o.add, o.ldadd, MLP_FP32);
+}
 
 SideArgs side(const void* p, int64_t ld, int64_t rows, int64_t cols) {
   return SideArgs{static_cast<const uint16_t*>(p), ld, rows, cols};
@@ -57,7 +67,7 @@ DenseWs dense_ws(int64_t M, int64_t K, int64_t N, int mode) {
 
 struct HeadWs {
   HeadPlan plan;
-  size_t lse2, row_loss, alpha, ok, part, pick, index, q, start, P, acc, partial, total;
+  size_t lse2, row_loss, alpha, ok, part, pick, index, q, start, P, ref, acc, partial, total;
   int keys;
   int64_t ldp;
 };
@@ -85,6 +95,7 @@ HeadWs head_ws(int64_t M, int64_t D, int64_t V, int top, int mode, bool teacher)
   if (mode == MLP_MODE_TRAIN) {
     w.ldp = (int64_t)round_up((size_t)w.plan.piece, 8);
     w.P = take((size_t)M * w.ldp * 2);
+    w.ref = take((size_t)M * w.plan.refs * 4);
     w.acc = take(w.plan.pieces > 1 ? (size_t)M * D * 4 : 0);
     size_t p = 0;
     for (int v0 = 0; v0 < V; v0 += w.plan.piece) {  // the last piece may differ
@@ -132,9 +143,16 @@ int run_head(bool distill, HeadArgs a, RowLossArgs r, const HeadWs& w, uint8_t* 
   a.nt = w.plan.nt;
   a.runs = w.plan.runs;
   a.per_run = w.plan.per_run;
+  uint16_t* P = reinterpret_cast<uint16_t*>(ws + w.P);
+  if (dW) {
+    a.P = P;
+    a.ldp = w.ldp;
+    a.keep = w.plan.piece;
+    a.ref = reinterpret_cast<float*>(ws + w.ref);
+  }
   hipError_t e;
   if (M > 0) {
-    e = launch(false, w.plan.large, side_aligned(a.h) && side_aligned(a.w), a, s);
+    e = launch(HEAD_LSE, w.plan.large, a, s);
     if (e != hipSuccess) return hip_fail(e, "log-sum-exp kernel launch");
   }
   r.partial = a.partial;
@@ -148,20 +166,19 @@ int run_head(bool distill, HeadArgs a, RowLossArgs r, const HeadWs& w, uint8_t* 
   e = launch_row_loss(r, s);
   if (e != hipSuccess) return hip_fail(e, "row loss kernel launch");
   if (!dW) return MLP_OK;
-  uint16_t* P = reinterpret_cast<uint16_t*>(ws + w.P);
   float* partial = reinterpret_cast<float*>(ws + w.partial);
   float* acc = reinterpret_cast<float*>(ws + w.acc);
   const int n_pieces = w.plan.pieces;
   for (int k = 0; k < n_pieces; ++k) {
     const int v0 = k * w.plan.piece, n = V - v0 < w.plan.piece ? V - v0 : w.plan.piece;
     if (M > 0) {
-      a.w = side(all.p + v0, all.ld, D, n);
-      a.V = n;
-      a.col0 = v0;
-      a.P = P;
-      a.ldp = w.ldp;
-      a.nt = (int)((n + (w.plan.large ? 255 : 127)) / (w.plan.large ? 256 : 128));
-      e = launch(true, w.plan.large, side_aligned(a.h) && side_aligned(a.w), a, s);
+      if (k > 0) {
+        a.w = side(all.p + v0, all.ld, D, n);
+        a.V = n;
+        a.col0 = v0;
+        a.nt = (int)((n + (w.plan.large ? 255 : 127)) / (w.plan.large ? 256 : 128));
+      }
+      e = launch(k == 0 ? HEAD_SCALE : HEAD_PROB, w.plan.large, a, s);
       if (e != hipSuccess) return hip_fail(e, "logit gradient kernel launch");
       // dH: pieces before the last add up in fp32
       GemmArgs g{};
@@ -184,7 +201,7 @@ int run_head(bool distill, HeadArgs a, RowLossArgs r, const HeadWs& w, uint8_t* 
         g.out.ldc = lddh;
         g.out.c_fp32 = dh_type == MLP_FP32;
       }
-      g.out.vec = four_wide(g.out.C, g.out.ldc, g.out.c_fp32 ? MLP_FP32 : MLP_BF16) && D % 4 == 0;
+      set_vec(g.out, D);
       e = launch_gemm(GEMM_DX, g, partial, s);
       if (e != hipSuccess) return hip_fail(e, "dH product launch");
     }
@@ -198,7 +215,7 @@ int run_head(bool distill, HeadArgs a, RowLossArgs r, const HeadWs& w, uint8_t* 
     g.out.C = static_cast<uint8_t*>(dW) + (size_t)v0 * type_size(dw_type);
     g.out.ldc = lddw;
     g.out.c_fp32 = dw_type == MLP_FP32;
-    g.out.vec = four_wide(g.out.C, lddw, dw_type);
+    set_vec(g.out, n);
     e = launch_gemm(GEMM_DW, g, partial, s);
     if (e != hipSuccess) return hip_fail(e, "dW product launch");
   }
@@ -327,7 +344,7 @@ int mlp_dense_forward(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_t
   g.out.C = Y;
   g.out.ldc = ldy;
   g.out.c_fp32 = y_type == MLP_FP32;
-  g.out.vec = four_wide(Y, ldy, y_type) && four_wide(R, ldr, y_type) && four_wide(g.out.stash, N, MLP_FP32);
+  set_vec(g.out, N);
   const hipError_t e = launch_gemm(GEMM_XW, g, static_cast<float*>(ws), static_cast<hipStream_t>(stream));
   return e == hipSuccess ? MLP_OK : hip_fail(e, "dense product launch");
 }
@@ -386,7 +403,7 @@ int mlp_dense_backward(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_
     g.out.C = dX;
     g.out.ldc = lddx;
     g.out.c_fp32 = dx_type == MLP_FP32;
-    g.out.vec = four_wide(dX, lddx, dx_type);
+    set_vec(g.out, K);
     e = launch_gemm(GEMM_DX, g, partial, s);
     if (e != hipSuccess) return hip_fail(e, "dX product launch");
   }
@@ -401,7 +418,7 @@ int mlp_dense_backward(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_
     g.out.C = dW;
     g.out.ldc = lddw;
     g.out.c_fp32 = dw_type == MLP_FP32;
-    g.out.vec = four_wide(dW, lddw, dw_type);
+    set_vec(g.out, N);
     e = launch_gemm(GEMM_DW, g, partial, s);
     if (e != hipSuccess) return hip_fail(e, "dW product launch");
   }

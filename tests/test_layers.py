@@ -338,8 +338,11 @@ def check_head(loss, rl, dH, dW, h, w, l, lse, e_l, q, index, live, T, gt, ents=
         return
     p = torch.exp(l - lse) * live[:, None]
     P = p.scatter_add(1, index, -(q * live[:, None]))
-    # P: the error of the exponent, q's own, then the rounding to bf16
-    e_P = p * (e_l + e_lse) + 32 * U * p
+    # P: the error of the exponent, q's own, then the rounding to bf16.  The
+    # first piece of the vocabulary passes through fp16 as 2^15 p / p_max, p_max
+    # the largest of a block of columns: half a step is 2^-11 of a normal value
+    # and 2^-25 of the smallest ones, that is 2^-40 p_max <= 2^-40.
+    e_P = p * (e_l + e_lse) + (32 * U + 2.0 ** -11) * p + 2.0 ** -40 * live[:, None]
     e_P = e_P.scatter_add(1, index, 64 * U * q) + HALF[BF] * P.abs()
     a = T / n
     ref, s = a * (P @ w.t()), a * (P.abs() @ w.abs().t())

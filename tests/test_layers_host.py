@@ -63,8 +63,8 @@ def test_workspace_sizes(ffmlp):
     assert d.workspace_bytes(8192) >= 8192 * 4096 * 2  # the rounded delta
     assert ffmlp.Dense(8, 8).workspace_bytes(8, ffmlp.MLP_MODE_INFER) == 0
     h = ffmlp.SoftmaxHead(2048, 1 << 17)
-    # the logits of 16384 tokens would take 8 GiB; a piece of them takes 512 MiB
-    assert h.workspace_bytes(16384) < 1 << 30
+    # the logits of 16384 tokens would take 8 GiB; a piece of them takes 1 GiB
+    assert h.workspace_bytes(16384) < 3 << 29
     # without gradients: sums per row and run, and where each 128 columns begin
     assert h.workspace_bytes(16384, ffmlp.MLP_MODE_INFER) < 64 << 20
     assert h.workspace_bytes(64, top=1024) > h.workspace_bytes(64)
