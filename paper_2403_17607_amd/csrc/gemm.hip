@@ -7,38 +7,71 @@ namespace ffmlp {
 
 namespace {
 
-constexpr int kWorkgroups = 512;  // two per CU
-
-struct TileSize { int bm, bn, bk; };
-TileSize tile_size(int tile) {
-  if (tile == GEMM_SQUARE) return {GemmSquare::BM, GemmSquare::BN, GemmSquare::BK};
-  if (tile == GEMM_LARGE) return {GemmLarge::BM, GemmLarge::BN, GemmLarge::BK};
-  if (tile == GEMM_MEDIUM) return {GemmMedium::BM, GemmMedium::BN, GemmMedium::BK};
-  return {GemmRows::BM, GemmRows::BN, GemmRows::BK};
-}
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// What a tile costs, in microseconds measured on an MI355X: a step of k of a
+// workgroup that has a CU to itself and of one that shares it, and the rest of
+// its life (first loads, epilogue), which shared CUs hide in part.  Shapes of
+// 2048 .. 8192 rows, 1024 .. 8192 columns and 1024 .. 32768 of k, both ways:
+//   8192 x 1024 over 4096 (X W): square 106, large 85, half 71, medium 89; with
+//     two splits and their sum large 82
+//   8192 x 8192 over 2048 (X W): square 265, large 240, half 285
+//   4096 x 1024 over 8192 (X^T dZ): square 191, half 104, medium 90; half with
+//     two splits and their sum 85
+//   1024 x 1024 over 1024 (X W): large 25, half 16, medium 12
+struct TileCost {
+  int tile, bm, bn, bk, per_cu;
+  double alone, shared, rest;
+};
+template <typename TL>
+constexpr TileCost tile_cost(int tile, int per_cu, double alone, double shared, double rest) {
+  return TileCost{tile, TL::BM, TL::BN, TL::BK, per_cu, alone, shared, rest};
+}
+constexpr TileCost kTiles[] = {
+    tile_cost<GemmSquare>(GEMM_SQUARE, 1, 1.60, 1.60, 16.0),
+    tile_cost<GemmLarge>(GEMM_LARGE, 2, 0.62, 0.90, 4.0),
+    tile_cost<GemmHalf>(GEMM_HALF, 2, 0.75, 1.05, 5.0),
+    tile_cost<GemmMedium>(GEMM_MEDIUM, 2, 0.42, 0.66, 4.0),
+    tile_cost<GemmRows>(GEMM_ROWS, 2, 0.30, 0.40, 3.0),
+};
+constexpr int kCUs = 256;
+
+// One side only: the large tile's short rows of k suit a side with k across
+// its rows (X W); 16-row tiles need rows on the m side.
+bool tile_suits(int tile, int form, int64_t M) {
+  if (tile == GEMM_LARGE) return form == GEMM_XW;
+  if (tile == GEMM_ROWS) return form != GEMM_DW && M <= GemmRows::BM;
+  return true;
+}
+
+bool few_rows(int form, int64_t M) { return form == GEMM_XW && M <= 8; }
 
 }  // namespace
 
 GemmPlan gemm_plan(int form, int64_t M, int64_t N, int64_t K) {
-  GemmPlan p{};
-  const int64_t large = cdiv(M, GemmLarge::BM) * cdiv(N, GemmLarge::BN);
-  p.tile = form != GEMM_DW && M <= GemmRows::BM ? GEMM_ROWS
-           : large < kWorkgroups / 4             ? GEMM_MEDIUM
-           : form == GEMM_XW                     ? GEMM_LARGE
-                                                 : GEMM_SQUARE;
-  const TileSize t = tile_size(p.tile);
-  p.mt = (int)cdiv(M, t.bm);
-  p.nt = (int)cdiv(N, t.bn);
-  const int64_t tiles = (int64_t)p.mt * p.nt;
-  // Splits fill the chip when the tiles do not, each over at least 256 of k.
-  int64_t s = (p.tile == GEMM_SQUARE ? kWorkgroups / 2 : kWorkgroups) / tiles, most = K / 256;
-  if (s > most) s = most;
-  if (s < 1) s = 1;
-  p.kper = K > 0 ? cdiv(cdiv(K, s), t.bk) * t.bk : t.bk;
-  p.splits = K > 0 ? (int)cdiv(K, p.kper) : 1;
-  p.partial_bytes = p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0;
-  return p;
+  GemmPlan best{};
+  if (few_rows(form, M)) return best;
+  double best_us = 0;
+  for (const TileCost& t : kTiles) {
+    if (!tile_suits(t.tile, form, M)) continue;
+    const int64_t mt = cdiv(M, t.bm), nt = cdiv(N, t.bn), tiles = mt * nt, slots = (int64_t)kCUs * t.per_cu;
+    const int64_t steps = cdiv(K > 0 ? K : 1, t.bk);
+    for (int64_t want = 1; want == 1 || (want <= 64 && want * 4 <= steps && tiles * want <= slots); want *= 2) {
+      const int64_t per = cdiv(steps, want), splits = cdiv(steps, per), n = tiles * splits;
+      const double us = (double)cdiv(n, slots) * ((double)per * (n > kCUs ? t.shared : t.alone) + t.rest) +
+                        (splits > 1 ? 5.0 + (double)(splits + 1) * (double)M * (double)N * 4e-6 / 4.5 : 0.0);
+      if (best_us == 0 || us < best_us) {
+        best_us = us;
+        best.tile = t.tile;
+        best.mt = (int)mt;
+        best.nt = (int)nt;
+        best.kper = per * t.bk;
+        best.splits = (int)splits;
+      }
+    }
+  }
+  best.partial_bytes = best.splits > 1 ? (size_t)best.splits * M * N * 4 : 0;
+  return best;
 }
 
 // The splits' partial sums added in order, then the epilogue.
@@ -51,7 +84,15 @@ __global__ __launch_bounds__(256) void split_sum_kernel(const float* partial, in
   const float* p = partial + m * N + n;
   f32x4 z = {0.f, 0.f, 0.f, 0.f};
   if ((N & 3) == 0) {
-    for (int s = 0; s < splits; ++s, p += M * N) z += *reinterpret_cast<const f32x4*>(p);
+    int s = 0;
+    for (; s + 4 <= splits; s += 4, p += 4 * M * N) {  // four loads in flight, added in order
+      f32x4 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const f32x4*>(p + k * M * N);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) z += v[k];
+    }
+    for (; s < splits; ++s, p += M * N) z += *reinterpret_cast<const f32x4*>(p);
   } else {
     for (int s = 0; s < splits; ++s, p += M * N)
 #pragma unroll
@@ -60,8 +101,11 @@ __global__ __launch_bounds__(256) void split_sum_kernel(const float* partial, in
   out4(o, m, n, N, z);
 }
 
+hipError_t launch_few_rows(const GemmArgs& a, hipStream_t s);
+
 hipError_t launch_gemm(int form, GemmArgs a, float* partial, hipStream_t s) {
   if (a.M <= 0 || a.N <= 0) return hipSuccess;
+  if (few_rows(form, a.M)) return launch_few_rows(a, s);
   const GemmPlan p = gemm_plan(form, a.M, a.N, a.K);
   a.mt = p.mt;
   a.nt = p.nt;
@@ -76,6 +120,91 @@ hipError_t launch_gemm(int form, GemmArgs a, float* partial, hipStream_t s) {
   const int64_t n = a.M * ((a.N + 3) / 4);
   hipLaunchKernelGGL(split_sum_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, partial, p.splits, a.M, a.N, a.out);
   return hipGetLastError();
+}
+
+// -------------------------------------------------------------- few rows --
+
+// Y = X W for MR <= 8 rows: W is read once and its products are made on the
+// vector units, so bandwidth and latency bound it (one row of 4096 x 4096: the
+// 32 MiB of W).  A workgroup owns 8 LPR columns; LPR lanes hold them as 16-byte
+// pieces, the wave's 64 / LPR groups take eight consecutive k each, the NW waves
+// every NW-th such block.  Then the groups' sums are added by shuffles and the
+// waves' in order through LDS.  LPR is chosen so that 256 workgroups or more
+// share N; those that share the 128 bytes of a line run on one chiplet.
+// Against the matrix-core kernel with splits (two launches), one row of 4096 x
+// 4096: FEW_RESULT.
+template <int MR, int NW, int LPR>
+__global__ __launch_bounds__(NW * 64) void few_rows_kernel(const GemmArgs a) {
+  constexpr int COLS = 8 * LPR, PER = 64 / COLS;  // workgroups of a line
+  __shared__ float sums[NW][MR][COLS];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // workgroup b runs on chiplet b % 8: its neighbour there is b + 8
+  const int b = blockIdx.x, at = (b / (8 * PER) * 8 + b % 8) * PER + b / 8 % PER;
+  const int n = at * COLS + 8 * (lane % LPR);
+  const int cols = a.N - n;  // of this lane
+  float acc[MR][8] = {};
+  if (cols > 0) {
+    for (int64_t k = (wave * (64 / LPR) + lane / LPR) * 8; k < a.K; k += NW * (64 / LPR) * 8) {
+      const int kn = a.K - k < 8 ? (int)(a.K - k) : 8;
+      u32x4 x[MR], w[8];
+      if (cols >= 8 && kn == 8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const u32x4_a2*>(a.n.p + (k + j) * a.n.ld + n);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          w[j] = u32x4{0u, 0u, 0u, 0u};
+          if (j < kn)
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              if (q < cols) w[j][q / 2] |= (uint32_t)a.n.p[(k + j) * a.n.ld + n + q] << (16 * (q & 1));
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < MR; ++m) x[m] = load8_bits(a.m.p + (m < a.M ? m : 0) * a.m.ld + k, kn);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float lo = bf16_lo(w[j][q]), hi = bf16_hi(w[j][q]);
+#pragma unroll
+          for (int m = 0; m < MR; ++m) {
+            const float v = j & 1 ? bf16_hi(x[m][j / 2]) : bf16_lo(x[m][j / 2]);
+            acc[m][2 * q] += v * lo;
+            acc[m][2 * q + 1] += v * hi;
+          }
+        }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+#pragma unroll
+      for (int d = LPR; d < 64; d *= 2) acc[m][q] += __shfl_xor(acc[m][q], d);
+      if (lane < LPR) sums[wave][m][8 * lane + q] = acc[m][q];
+    }
+  __syncthreads();
+  const int m = threadIdx.x / (COLS / 4), c = 4 * (threadIdx.x % (COLS / 4));
+  if (m >= MR || m >= a.M || at * COLS + c >= a.N) return;
+  f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < NW; ++w) z += *reinterpret_cast<const f32x4*>(&sums[w][m][c]);
+  out4(a.out, m, at * COLS + c, a.N, z);
+}
+
+template <int LPR>
+hipError_t launch_few_rows_cols(const GemmArgs& a, hipStream_t s) {
+  constexpr int COLS = 8 * LPR, PER = 64 / COLS;
+  const dim3 grid((unsigned)(cdiv(a.N, COLS * 8 * PER) * 8 * PER));  // whole lines on eight chiplets
+  if (a.M <= 1) hipLaunchKernelGGL((few_rows_kernel<1, 16, LPR>), grid, dim3(1024), 0, s, a);
+  else if (a.M <= 2) hipLaunchKernelGGL((few_rows_kernel<2, 16, LPR>), grid, dim3(1024), 0, s, a);
+  else if (a.M <= 4) hipLaunchKernelGGL((few_rows_kernel<4, 8, LPR>), grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((few_rows_kernel<8, 8, LPR>), grid, dim3(512), 0, s, a);
+  return hipGetLastError();
+}
+hipError_t launch_few_rows(const GemmArgs& a, hipStream_t s) {
+  return a.N >= 64 * 256 ? launch_few_rows_cols<8>(a, s) : a.N >= 32 * 256 ? launch_few_rows_cols<4>(a, s) : launch_few_rows_cols<2>(a, s);
 }
 
 // ------------------------------------------------------------ column sums --
@@ -123,7 +252,7 @@ __global__ __launch_bounds__(256) void delta_kernel(const DeltaArgs a) {
 }
 
 int delta_parts(int64_t M, int N) {
-  const int64_t want = cdiv(2 * kWorkgroups, cdiv(N, 512)), most = cdiv(M, 16);
+  const int64_t want = cdiv(4 * kCUs, cdiv(N, 512)), most = cdiv(M, 16);
   return (int)(want < most ? want : most < 1 ? 1 : most);
 }
 

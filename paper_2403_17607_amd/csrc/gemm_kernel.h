@@ -504,11 +504,12 @@ hipError_t launch_gemm_tile(GemmArgs a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Workgroup tiles.  GemmLarge: two workgroups per CU (72 KiB of LDS each), so
-// that one's epilogue hides behind the other's products.  GemmSquare: one, with
-// fewer bytes per product and 128-byte rows of k.
+// Workgroup tiles.  GemmSquare: one workgroup per CU (128 KiB of LDS), fewest
+// bytes per product, 128-byte rows of k.  The others: two per CU, so that one's
+// epilogue hides behind the other's products.  gemm.hip chooses by what they cost.
 typedef GemmTile<128, 256, 32, 2, 2, 3> GemmLarge;
 typedef GemmTile<256, 256, 64, 2, 4, 2> GemmSquare;
+typedef GemmTile<128, 128, 64, 2, 2, 2> GemmHalf;
 typedef GemmTile<64, 128, 64, 2, 2, 3> GemmMedium;
 typedef GemmTile<16, 128, 64, 1, 4, 4> GemmRows;
 

@@ -10,7 +10,7 @@ constexpr int64_t kPieceElems = (int64_t)1 << 29;  // P of a piece: 1 GiB
 
 HeadPlan head_plan(int64_t M, int64_t, int64_t V) {
   HeadPlan p{};
-  p.large = cdiv(M, GemmLarge::BM) * cdiv(V, GemmLarge::BN) >= 128;
+  p.large = cdiv(M, GemmLarge::BM) * cdiv(V, GemmLarge::BN) >= 512;
   p.mt = (int)cdiv(M, p.large ? GemmLarge::BM : GemmMedium::BM);
   p.nt = (int)cdiv(V, p.large ? GemmLarge::BN : GemmMedium::BN);
   int64_t runs = 512 / (p.mt > 0 ? p.mt : 1);

@@ -17,13 +17,12 @@ namespace ffmlp {
 
 namespace {
 
-constexpr int kNormParts = 256;  // one workgroup per CU in the backward pass
-
 template <bool F32> struct Elem { typedef uint16_t type; };
 template <> struct Elem<true> { typedef float type; };
 
-// Sum over the G lanes (aligned groups of a wave) that hold a row, or over
-// the workgroup (G = 256; `lds` has 8 floats, two per wave in turn).
+// Sum over the G consecutive threads that hold a row, in a fixed order: by
+// shuffles, and through LDS (two floats per wave) where they are several waves,
+// which all of the workgroup then passes together.
 template <int G>
 __device__ __forceinline__ void row_sum2(float& a, float& b, float* lds) {
 #pragma unroll
@@ -31,7 +30,7 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, float* lds) {
     a += __shfl_xor(a, m);
     b += __shfl_xor(b, m);
   }
-  if constexpr (G == 256) {
+  if constexpr (G > 64) {
     const int wave = threadIdx.x >> 6;
     __syncthreads();  // the last sums have been read
     if ((threadIdx.x & 63) == 0) {
@@ -39,8 +38,13 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, float* lds) {
       lds[2 * wave + 1] = b;
     }
     __syncthreads();
-    a = (lds[0] + lds[2]) + (lds[4] + lds[6]);
-    b = (lds[1] + lds[3]) + (lds[5] + lds[7]);
+    a = b = 0.f;
+    const float* of = lds + 2 * (threadIdx.x / G) * (G / 64);
+#pragma unroll
+    for (int w = 0; w < G / 64; ++w) {
+      a += of[2 * w];
+      b += of[2 * w + 1];
+    }
   }
 }
 
@@ -69,8 +73,125 @@ __device__ __forceinline__ void row_stats(const float (&x)[J][8], int lane, int 
   rstd = 1.f / __builtin_sqrtf(v / (float)N + eps);
 }
 
+// Rows of whole pieces (N a multiple of 8) go through buffer descriptors that
+// begin at a wave's first row: a lane's offsets stay the same from row to row
+// and lanes past N are out of range (they read zeros and store nothing), so no
+// branch and no address arithmetic stands between the loads of a row.
+template <bool F32, int G, int J>
+struct WholeRows {
+  static constexpr int SIZE = F32 ? 4 : 2;
+  const uint8_t* p;
+  int64_t ld;
+  uint32_t voff[J];
+  rsrc_t r;
+  __device__ __forceinline__ void init(const void* base, int64_t stride, int N) {
+    p = static_cast<const uint8_t*>(base);
+    ld = stride;
+    const int lane = threadIdx.x % G, grp = (threadIdx.x & 63) / G;  // grp: 0 where G >= 64
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int c = 8 * (j * G + lane);
+      voff[j] = c < N ? (uint32_t)((grp * stride + c) * SIZE) : kOOB;
+    }
+  }
+  // `row`: the wave's first row, wave-uniform; rows M and past it do not exist.
+  __device__ __forceinline__ void at(int64_t row, int64_t M, int N) {
+    constexpr int ROWS = G < 64 ? 64 / G : 1;
+    const int64_t left = M - row, rows = left < ROWS ? left : ROWS;
+    r = make_rsrc(p + row * ld * SIZE, rows <= 0 ? 0 : ((rows - 1) * ld + N) * SIZE);
+  }
+  struct Raw {
+    u32x4 x[F32 ? 2 : 1];
+  };
+  __device__ __forceinline__ Raw load(int j) const {
+    Raw v;
+    v.x[0] = bload128(r, voff[j], 0);
+    if constexpr (F32) v.x[1] = bload128(r, voff[j] + 16, 0);
+    return v;
+  }
+  static __device__ __forceinline__ void widen(const Raw& v, float (&f)[8]) {
+    if constexpr (F32) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f[q] = __uint_as_float(v.x[0][q]);
+        f[q + 4] = __uint_as_float(v.x[1][q]);
+      }
+    } else {
+      widen8(v.x[0], f);
+    }
+  }
+  __device__ __forceinline__ void store(int j, const float (&f)[8]) const {
+    if constexpr (F32) {
+      bstore128<false>(__builtin_bit_cast(u32x4, f32x4{f[0], f[1], f[2], f[3]}), r, voff[j], 0);
+      bstore128<false>(__builtin_bit_cast(u32x4, f32x4{f[4], f[5], f[6], f[7]}), r, voff[j] + 16, 0);
+    } else {
+      bstore128<false>(u32x4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])}, r, voff[j], 0);
+    }
+  }
+};
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+// gamma (ones where it is NULL) or beta (zeros) in LDS, zeros past N.
+__device__ __forceinline__ void fill_columns(float* dst, int cols, const float* src, int N, float missing) {
+  for (int c = threadIdx.x; c < cols; c += blockDim.x) dst[c] = c < N ? (src ? src[c] : missing) : 0.f;
+}
+__device__ __forceinline__ void lds8(const float* p, float (&v)[8]) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    v[q] = a[q];
+    v[q + 4] = b[q];
+  }
+}
+
 }  // namespace
 
+template <int G, int J, bool X32, bool Y32>
+__global__ __launch_bounds__(256) void norm_fwd_whole_kernel(const NormArgs a) {
+  __shared__ float lds[8];
+  const int lane = threadIdx.x % G;
+  constexpr int PER = 256 / G, WPR = G < 64 ? 64 / G : 1;  // rows of a workgroup, of a wave
+  WholeRows<X32, G, J> X;
+  WholeRows<Y32, G, J> Y;
+  X.init(a.X, a.ldx, a.N);
+  Y.init(a.Y, a.ldy, a.N);
+  const int wave_row = G <= 64 ? (int)(threadIdx.x >> 6) * WPR : 0;
+  for (int64_t first = (int64_t)blockIdx.x * PER; first < a.M; first += (int64_t)gridDim.x * PER) {
+    const int64_t row0 = uniform(first + wave_row), row = row0 + (threadIdx.x & 63) / G;
+    X.at(row0, a.M, a.N);
+    Y.at(row0, a.M, a.N);
+    typename WholeRows<X32, G, J>::Raw raw[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) raw[j] = X.load(j);
+    float g[J][8], b[J][8], x[J][8];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {  // in flight with the row
+      const int c = 8 * (j * G + lane);
+      if (a.gamma) load8(a.gamma + (c < a.N ? c : a.N - 8), 8, g[j]);
+      if (a.beta) load8(a.beta + (c < a.N ? c : a.N - 8), 8, b[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j) X.widen(raw[j], x[j]);
+    float mean, rstd;
+    row_stats<G, J>(x, lane, a.N, a.eps, lds, mean, rstd);
+    if (a.stats && lane == 0 && row < a.M) *reinterpret_cast<f32x2*>(a.stats + 2 * row) = f32x2{mean, rstd};
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      float y[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        y[q] = (x[j][q] - mean) * rstd;
+        if (a.gamma) y[q] *= g[j][q];
+        if (a.beta) y[q] += b[j][q];
+      }
+      Y.store(j, y);
+    }
+  }
+}
+
+// Rows of any length.
 template <int G, int J, bool X32, bool Y32>
 __global__ __launch_bounds__(256) void norm_fwd_kernel(const NormArgs a) {
   typedef typename Elem<X32>::type TX;
@@ -108,81 +229,41 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(const NormArgs a) {
   }
 }
 
-// Each group of G lanes takes rows blockIdx + k gridDim ... of its own and
-// keeps the sums for dgamma and dbeta of its columns in registers; at the end
-// the workgroup's groups are added in a fixed order and written as one part.
-template <int G, int J, bool X32, bool DY32>
-__global__ __launch_bounds__(256) void norm_bwd_kernel(const NormArgs a) {
-  typedef typename Elem<X32>::type TX;
-  typedef typename Elem<DY32>::type TD;
-  constexpr int GROUPS = 256 / G, COLS = 8 * J * G;
-  __shared__ float lds[8];
-  __shared__ float sums[GROUPS > 1 ? COLS : 1];
-  const int lane = threadIdx.x % G, grp = threadIdx.x / G;
-  float dg[J][8] = {}, db[J][8] = {};
-  for (int64_t row = (int64_t)blockIdx.x * GROUPS + grp; row < a.M; row += (int64_t)gridDim.x * GROUPS) {
-    const TX* X = static_cast<const TX*>(a.X) + row * a.ldx;
-    const TD* D = static_cast<const TD*>(a.dY) + row * a.lddy;
-    float x[J][8], d[J][8];
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int c = 8 * (j * G + lane);
-      load8(X + c, a.N - c, x[j]);
-      load8(D + c, a.N - c, d[j]);
-    }
-    const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
-    float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int c = 8 * (j * G + lane), n = a.N - c;
-      float g[8];
-      if (a.gamma && n > 0) load8(a.gamma + c, n, g);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const float xh = (x[j][q] - st[0]) * st[1];
-        dg[j][q] += q < n ? d[j][q] * xh : 0.f;
-        db[j][q] += d[j][q];
-        const float u = a.gamma ? (q < n ? d[j][q] * g[q] : 0.f) : d[j][q];
-        x[j][q] = xh;
-        d[j][q] = u;
-        s1 += u;
-        s2 += q < n ? u * xh : 0.f;
-      }
-    }
-    row_sum2<G>(s1, s2, lds);
-    s1 /= (float)a.N;
-    s2 /= (float)a.N;
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int c = 8 * (j * G + lane), n = a.N - c;
-      if (n <= 0) continue;
-#pragma unroll
-      for (int q = 0; q < 8; ++q) d[j][q] = st[1] * (d[j][q] - s1 - x[j][q] * s2);
-      if (a.dx_fp32) store8(static_cast<float*>(a.dX) + row * a.lddx + c, n, d[j]);
-      else store8(static_cast<uint16_t*>(a.dX) + row * a.lddx + c, n, d[j]);
-    }
-  }
+// Threads of a backward workgroup, as many as its registers allow: they share
+// one part of the sums for dgamma and dbeta.
+template <int G, int J> constexpr int norm_bwd_threads() { return G == 64 && J == 2 ? 768 : 1024; }
+
+// A workgroup's sums for dgamma and dbeta as one part: those of its waves (or
+// of its groups of several waves) added in a fixed order.
+template <int G, int J>
+__device__ __forceinline__ void write_part(const NormArgs& a, float (&dg)[J][8], float (&db)[J][8], float* sums) {
+  constexpr int UNIT = G < 64 ? 64 : G, UNITS = norm_bwd_threads<G, J>() / UNIT;
+  const int lane = threadIdx.x % G, unit = threadIdx.x / UNIT;
   float* part = a.partial + (int64_t)blockIdx.x * 2 * a.N;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
     float(&v)[J][8] = w ? db : dg;
-    if constexpr (GROUPS > 1) {
-      for (int k = GROUPS - 1; k >= 0; --k) {  // the last group first, group 0 adds and writes
+    if constexpr (UNITS > 1) {
+#pragma unroll
+      for (int m = G; m < 64; m *= 2)  // the groups of a wave
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[0][q] += __shfl_xor(v[0][q], m);
+      for (int k = UNITS - 1; k >= 0; --k) {  // the last one first, the first adds and writes
         __syncthreads();
-        if (grp == k) {
+        if (unit == k && threadIdx.x % UNIT < G) {
 #pragma unroll
           for (int j = 0; j < J; ++j)
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
               float& s = sums[8 * (j * G + lane) + q];
-              v[j][q] += k == GROUPS - 1 ? 0.f : s;
+              v[j][q] += k == UNITS - 1 ? 0.f : s;
               s = v[j][q];
             }
         }
       }
       __syncthreads();
     }
-    if (grp == 0)
+    if (threadIdx.x < G)
 #pragma unroll
       for (int j = 0; j < J; ++j) {
         const int c = 8 * (j * G + lane);
@@ -191,6 +272,155 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(const NormArgs a) {
           if (c + q < a.N) part[(int64_t)w * a.N + c + q] = v[j][q];
       }
   }
+}
+
+// What a piece adds to the sums: of its row (s1 = sum u, s2 = sum u xh) and of
+// its columns.  Past N dy is 0, and so is what it adds to a row's sums; the
+// columns' own sums there are not written.
+__device__ __forceinline__ void bwd_sums(const float (&x)[8], const float (&d)[8], const float (&g)[8], const f32x2& st, float (&dg)[8],
+                                         float (&db)[8], float& s1, float& s2) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const float xh = (x[q] - st[0]) * st[1], u = d[q] * g[q];
+    dg[q] += d[q] * xh;
+    db[q] += d[q];
+    s1 += u;
+    s2 += u * xh;
+  }
+}
+__device__ __forceinline__ void bwd_dx(const float (&x)[8], float (&d)[8], const float (&g)[8], const f32x2& st, float s1, float s2) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const float xh = (x[q] - st[0]) * st[1];
+    d[q] = st[1] * (d[q] * g[q] - s1 - xh * s2);
+  }
+}
+
+// Each group of G lanes takes rows blockIdx + k gridDim ... of its own and
+// keeps the sums for dgamma and dbeta of its columns in registers, gamma being
+// in LDS.  bf16 pieces stay packed until they are used; where registers allow
+// (J <= 2), a group asks for its next row before it works on the current one.
+template <int G, int J, bool X32, bool DY32, bool DX32>
+__global__ __launch_bounds__((norm_bwd_threads<G, J>())) void norm_bwd_whole_kernel(const NormArgs a) {
+  constexpr int NTHR = norm_bwd_threads<G, J>(), PER = NTHR / G, COLS = 8 * J * G, WPR = G < 64 ? 64 / G : 1;
+  constexpr bool AHEAD = J == 1 || (J == 2 && G <= 64 && !X32 && !DY32);
+  __shared__ float lds[32];
+  __shared__ __align__(16) float gamma[COLS];
+  __shared__ float sums[PER > 1 ? COLS : 1];
+  const int lane = threadIdx.x % G;
+  fill_columns(gamma, COLS, a.gamma, a.N, 1.f);
+  __syncthreads();
+  WholeRows<X32, G, J> X;
+  WholeRows<DY32, G, J> D;
+  WholeRows<DX32, G, J> O;
+  X.init(a.X, a.ldx, a.N);
+  D.init(a.dY, a.lddy, a.N);
+  O.init(a.dX, a.lddx, a.N);
+  float dg[J][8] = {}, db[J][8] = {};
+  typename WholeRows<X32, G, J>::Raw nx[J];
+  typename WholeRows<DY32, G, J>::Raw nd[J];
+  f32x2 nst;
+  const int wave_row = G <= 64 ? (int)(threadIdx.x >> 6) * WPR : threadIdx.x / G, in_wave = G < 64 ? (threadIdx.x & 63) / G : 0;
+  const auto fetch = [&](int64_t row0) {
+    X.at(row0, a.M, a.N);
+    D.at(row0, a.M, a.N);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      nx[j] = X.load(j);
+      nd[j] = D.load(j);
+    }
+    const int64_t row = row0 + in_wave;
+    nst = *reinterpret_cast<const f32x2*>(a.stats + 2 * (row < a.M ? row : a.M - 1));
+  };
+  const int64_t step = (int64_t)gridDim.x * PER;
+  int64_t first = (int64_t)blockIdx.x * PER;
+  if (AHEAD) fetch(uniform(first + wave_row));
+  for (; first < a.M; first += step) {
+    const int64_t row0 = uniform(first + wave_row);
+    if (!AHEAD) fetch(row0);
+    typename WholeRows<X32, G, J>::Raw px[J];
+    typename WholeRows<DY32, G, J>::Raw pd[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      px[j] = nx[j];
+      pd[j] = nd[j];
+    }
+    const f32x2 st = nst;
+    if (AHEAD) fetch(uniform(first + step + wave_row));
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      float g[8], x[8], d[8];
+      lds8(gamma + 8 * (j * G + lane), g);
+      X.widen(px[j], x);
+      D.widen(pd[j], d);
+      bwd_sums(x, d, g, st, dg[j], db[j], s1, s2);
+    }
+    row_sum2<G>(s1, s2, lds);
+    s1 /= (float)a.N;
+    s2 /= (float)a.N;
+    O.at(row0, a.M, a.N);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      float g[8], x[8], d[8];
+      lds8(gamma + 8 * (j * G + lane), g);
+      X.widen(px[j], x);
+      D.widen(pd[j], d);
+      bwd_dx(x, d, g, st, s1, s2);
+      O.store(j, d);
+    }
+  }
+  write_part<G, J>(a, dg, db, sums);
+}
+
+// The same for rows of any length.
+template <int G, int J, bool X32, bool DY32>
+__global__ __launch_bounds__((norm_bwd_threads<G, J>())) void norm_bwd_kernel(const NormArgs a) {
+  typedef typename Elem<X32>::type TX;
+  typedef typename Elem<DY32>::type TD;
+  constexpr int NTHR = norm_bwd_threads<G, J>(), PER = NTHR / G, COLS = 8 * J * G;
+  __shared__ float lds[32];
+  __shared__ __align__(16) float gamma[COLS];
+  __shared__ float sums[PER > 1 ? COLS : 1];
+  const int lane = threadIdx.x % G, grp = threadIdx.x / G;
+  fill_columns(gamma, COLS, a.gamma, a.N, 1.f);
+  __syncthreads();
+  float dg[J][8] = {}, db[J][8] = {};
+  for (int64_t first = (int64_t)blockIdx.x * PER; first < a.M; first += (int64_t)gridDim.x * PER) {
+    const bool in = first + grp < a.M;  // all groups pass the sums below together
+    const int64_t row = in ? first + grp : a.M - 1;
+    const TX* X = static_cast<const TX*>(a.X) + row * a.ldx;
+    const TD* D = static_cast<const TD*>(a.dY) + row * a.lddy;
+    float x[J][8], d[J][8];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int c = 8 * (j * G + lane);
+      load8(X + c, in ? a.N - c : 0, x[j]);
+      load8(D + c, in ? a.N - c : 0, d[j]);
+    }
+    const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      float g[8];
+      lds8(gamma + 8 * (j * G + lane), g);
+      bwd_sums(x[j], d[j], g, st, dg[j], db[j], s1, s2);
+    }
+    row_sum2<G>(s1, s2, lds);
+    s1 /= (float)a.N;
+    s2 /= (float)a.N;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int c = 8 * (j * G + lane), n = a.N - c;
+      float g[8];
+      lds8(gamma + c, g);
+      bwd_dx(x[j], d[j], g, st, s1, s2);
+      if (n <= 0 || !in) continue;
+      if (a.dx_fp32) store8(static_cast<float*>(a.dX) + row * a.lddx + c, n, d[j]);
+      else store8(static_cast<uint16_t*>(a.dX) + row * a.lddx + c, n, d[j]);
+    }
+  }
+  write_part<G, J>(a, dg, db, sums);
 }
 
 // ---- rows that do not fit the registers of a workgroup: three passes over a
@@ -337,40 +567,44 @@ hipError_t by_types(bool a32, bool b32, F&& f) {
   return b32 ? f(std::false_type{}, std::true_type{}) : f(std::false_type{}, std::false_type{});
 }
 
-// f(G, J): the fewest lanes and pieces that hold a row of N; false if none does.
-template <typename F>
-bool by_row(int N, F&& f) {
-  using std::integral_constant;
+// f(G, J): the lanes and pieces that hold a row of N; false if none do.  The
+// backward pass spreads long rows over more lanes, for its two sums per column.
 #define FFMLP_ROW(G, J) \
-  if (N <= 8 * G * J) { f(integral_constant<int, G>{}, integral_constant<int, J>{}); return true; }
-  FFMLP_ROW(8, 1)
-  FFMLP_ROW(16, 1)
-  FFMLP_ROW(32, 1)
-  FFMLP_ROW(64, 1)
-  FFMLP_ROW(64, 2)
-  FFMLP_ROW(64, 4)
-  FFMLP_ROW(256, 2)
-  FFMLP_ROW(256, 4)
-  FFMLP_ROW(256, 8)
-#undef FFMLP_ROW
+  if (N <= 8 * G * J) { f(std::integral_constant<int, G>{}, std::integral_constant<int, J>{}); return true; }
+template <typename F>
+bool by_row_forward(int N, F&& f) {
+  FFMLP_ROW(8, 1) FFMLP_ROW(16, 1) FFMLP_ROW(32, 1) FFMLP_ROW(64, 1) FFMLP_ROW(64, 2) FFMLP_ROW(64, 4)
+  FFMLP_ROW(256, 2) FFMLP_ROW(256, 4) FFMLP_ROW(256, 8)
   return false;
 }
+template <typename F>
+bool by_row_backward(int N, F&& f) {
+  FFMLP_ROW(8, 1) FFMLP_ROW(16, 1) FFMLP_ROW(32, 1) FFMLP_ROW(64, 1) FFMLP_ROW(64, 2) FFMLP_ROW(256, 1)
+  FFMLP_ROW(512, 1) FFMLP_ROW(1024, 1) FFMLP_ROW(1024, 2)
+  return false;
+}
+#undef FFMLP_ROW
 
 }  // namespace
 
 int norm_parts(int64_t M, int N) {
-  int groups = 1;
-  const bool held = by_row(N, [&](auto g, auto) { groups = 256 / decltype(g)::value; });
-  const int64_t most = held ? (M + groups - 1) / groups : (M + 15) / 16;
-  return (int)(most < 1 ? 1 : most < kNormParts ? most : kNormParts);
+  int rows = 16;  // that a workgroup takes at a time
+  by_row_backward(N, [&](auto g, auto j) {
+    constexpr int G = decltype(g)::value;
+    rows = norm_bwd_threads<G, decltype(j)::value>() / G;
+  });
+  const int64_t p = (M + rows - 1) / rows;
+  return (int)(p < 1 ? 1 : p < 256 ? p : 256);  // one workgroup per CU
 }
 
 hipError_t launch_norm_forward(const NormArgs& a, hipStream_t s) {
   return by_types(a.x_fp32, a.y_fp32, [&](auto x32, auto y32) {
     constexpr bool X = decltype(x32)::value, Y = decltype(y32)::value;
-    const bool held = by_row(a.N, [&](auto g, auto j) {
+    const bool held = by_row_forward(a.N, [&](auto g, auto j) {
       constexpr int G = decltype(g)::value, J = decltype(j)::value, R = 256 / G;
-      hipLaunchKernelGGL((norm_fwd_kernel<G, J, X, Y>), dim3(norm_grid((a.M + R - 1) / R)), dim3(256), 0, s, a);
+      const dim3 grid(norm_grid((a.M + R - 1) / R));
+      if (a.N % 8 == 0) hipLaunchKernelGGL((norm_fwd_whole_kernel<G, J, X, Y>), grid, dim3(256), 0, s, a);
+      else hipLaunchKernelGGL((norm_fwd_kernel<G, J, X, Y>), grid, dim3(256), 0, s, a);
     });
     if (!held) hipLaunchKernelGGL((norm_fwd_long_kernel<X, Y>), dim3(norm_grid(a.M)), dim3(256), 0, s, a);
     return hipGetLastError();
@@ -380,9 +614,12 @@ hipError_t launch_norm_forward(const NormArgs& a, hipStream_t s) {
 hipError_t launch_norm_backward(const NormArgs& a, hipStream_t s) {
   const hipError_t e = by_types(a.x_fp32, a.dy_fp32, [&](auto x32, auto d32) {
     constexpr bool X = decltype(x32)::value, D = decltype(d32)::value;
-    const bool held = by_row(a.N, [&](auto g, auto j) {
+    const bool held = by_row_backward(a.N, [&](auto g, auto j) {
       constexpr int G = decltype(g)::value, J = decltype(j)::value;
-      hipLaunchKernelGGL((norm_bwd_kernel<G, J, X, D>), dim3((unsigned)a.parts), dim3(256), 0, s, a);
+      const dim3 grid((unsigned)a.parts), block(norm_bwd_threads<G, J>());
+      if (a.N % 8 != 0) hipLaunchKernelGGL((norm_bwd_kernel<G, J, X, D>), grid, block, 0, s, a);
+      else if (a.dx_fp32) hipLaunchKernelGGL((norm_bwd_whole_kernel<G, J, X, D, true>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((norm_bwd_whole_kernel<G, J, X, D, false>), grid, block, 0, s, a);
     });
     if (!held) {  // the columns first: dX may be dY
       hipLaunchKernelGGL((norm_cols_long_kernel<X, D>), dim3((unsigned)((a.N + 511) / 512), (unsigned)a.parts), dim3(256), 0, s, a);

@@ -9,19 +9,22 @@ namespace ffmlp {
 
 typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 
-__device__ __forceinline__ void load8(const uint16_t* p, int n, float (&v)[8]) {
-  if (n >= 8) {
-    const u32x4 x = *reinterpret_cast<const u32x4_a2*>(p);
+__device__ __forceinline__ u32x4 load8_bits(const uint16_t* p, int n) {
+  if (n >= 8) return *reinterpret_cast<const u32x4_a2*>(p);
+  u32x4 x = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      v[2 * q] = bf16_lo(x[q]);
-      v[2 * q + 1] = bf16_hi(x[q]);
-    }
-  } else {
+  for (int q = 0; q < 8; ++q)
+    if (q < n) x[q / 2] |= (uint32_t)p[q] << (16 * (q & 1));
+  return x;
+}
+__device__ __forceinline__ void widen8(const u32x4& x, float (&v)[8]) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = q < n ? __uint_as_float((uint32_t)p[q] << 16) : 0.f;
+  for (int q = 0; q < 4; ++q) {
+    v[2 * q] = bf16_lo(x[q]);
+    v[2 * q + 1] = bf16_hi(x[q]);
   }
 }
+__device__ __forceinline__ void load8(const uint16_t* p, int n, float (&v)[8]) { widen8(load8_bits(p, n), v); }
 __device__ __forceinline__ void load8(const float* p, int n, float (&v)[8]) {
   if (n >= 8) {
     const f32x4 a = *reinterpret_cast<const f32x4_a4*>(p), b = *reinterpret_cast<const f32x4_a4*>(p + 4);

@@ -87,7 +87,25 @@ def _dim(n, name) -> int:
     return n
 
 
+def _run(fn, dev, *args) -> None:
+    """Call fn(*args, stream) with `dev` as the current device."""
+    if dev.index is None or dev.index == torch.cuda.current_device():
+        rc = fn(*args, _base._stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, _base._stream(dev))
+    if rc != 0:
+        _base._check(rc)
+
+
 class _Layer:
+    _need = (None, 0)  # the last workspace size asked for, with its arguments
+
+    def _ws_bytes(self, *key) -> int:
+        if self._need[0] != key:
+            self._need = (key, self.workspace_bytes(*key))
+        return self._need[1]
+
     def workspace_bytes(self, M: int, mode: int = _base.MLP_MODE_TRAIN) -> int:
         raise NotImplementedError
 
@@ -123,11 +141,9 @@ class LayerNorm(_Layer):
         Y, ldy = _out(Y, "Y", M, n, dtype or X.dtype, dev)
         if stats is not None:
             _base._require(stats, "stats", torch.float32, shape=(M, 2), device=dev)
-        with torch.cuda.device(dev):
-            _base._check(_base.lib().mlp_layer_norm_forward(
-                X.data_ptr(), _TYPES[X.dtype], ldx, _vector(gamma, "gamma", n, dev), _vector(beta, "beta", n, dev),
-                Y.data_ptr(), _TYPES[Y.dtype], ldy, None if stats is None else stats.data_ptr(), M, n, self.eps,
-                _base._stream(dev)))
+        _run(
+            _base.lib().mlp_layer_norm_forward, dev, X.data_ptr(), _TYPES[X.dtype], ldx, _vector(gamma, "gamma", n, dev), _vector(beta, "beta", n, dev),
+            Y.data_ptr(), _TYPES[Y.dtype], ldy, None if stats is None else stats.data_ptr(), M, n, self.eps)
         return Y
 
     def backward(self, X, gamma, stats, dY, ws, dX=None, dgamma=None, dbeta=None, dtype=None):
@@ -140,11 +156,10 @@ class LayerNorm(_Layer):
         dX, lddx = _out(dX, "dX", M, n, dtype or X.dtype, dev)
         dgamma = torch.empty(n, device=dev) if dgamma is None else dgamma
         dbeta = torch.empty(n, device=dev) if dbeta is None else dbeta
-        with torch.cuda.device(dev):
-            _base._check(_base.lib().mlp_layer_norm_backward(
-                X.data_ptr(), _TYPES[X.dtype], ldx, _vector(gamma, "gamma", n, dev), stats.data_ptr(), dY.data_ptr(),
-                _TYPES[dY.dtype], lddy, dX.data_ptr(), _TYPES[dX.dtype], lddx, _vector(dgamma, "dgamma", n, dev),
-                _vector(dbeta, "dbeta", n, dev), M, n, self._ws(ws, self.workspace_bytes(M), dev), _base._stream(dev)))
+        _run(
+            _base.lib().mlp_layer_norm_backward, dev, X.data_ptr(), _TYPES[X.dtype], ldx, _vector(gamma, "gamma", n, dev), stats.data_ptr(), dY.data_ptr(),
+            _TYPES[dY.dtype], lddy, dX.data_ptr(), _TYPES[dX.dtype], lddx, _vector(dgamma, "dgamma", n, dev),
+            _vector(dbeta, "dbeta", n, dev), M, n, self._ws(ws, self._ws_bytes(M), dev))
         return dX, dgamma, dbeta
 
 
@@ -188,12 +203,11 @@ class Dense(_Layer):
         if stash is not None:
             _base._require(stash, "stash", torch.float32, shape=(M, n), device=dev)
         L = _base.lib()
-        with torch.cuda.device(dev):
-            _base._check(L.mlp_dense_forward(
-                X.data_ptr(), ldx, W.data_ptr(), ldw, _vector(bias, "bias", n, dev), self.activation,
-                None if residual is None else residual.data_ptr(), ldr, Y.data_ptr(), _TYPES[Y.dtype], ldy,
-                None if stash is None else stash.data_ptr(), M, k, n,
-                self._ws(ws, self.workspace_bytes(M, _base.MLP_MODE_INFER), dev), _base._stream(dev)))
+        _run(
+            L.mlp_dense_forward, dev, X.data_ptr(), ldx, W.data_ptr(), ldw, _vector(bias, "bias", n, dev), self.activation,
+            None if residual is None else residual.data_ptr(), ldr, Y.data_ptr(), _TYPES[Y.dtype], ldy,
+            None if stash is None else stash.data_ptr(), M, k, n,
+            self._ws(ws, self._ws_bytes(M, _base.MLP_MODE_INFER), dev))
         return Y
 
     def backward(self, W, X, dY, ws, stash=None, dX=None, dW=None, db=None, dtype=torch.float32, input_gradient=True):
@@ -215,12 +229,11 @@ class Dense(_Layer):
         dW, lddw = _out(dW, "dW", k, n, dtype, dev)
         db = torch.empty(n, device=dev) if db is None else db
         L = _base.lib()
-        with torch.cuda.device(dev):
-            _base._check(L.mlp_dense_backward(
-                X.data_ptr(), ldx, W.data_ptr(), ldw, self.activation, None if stash is None else stash.data_ptr(),
-                dY.data_ptr(), _TYPES[dY.dtype], lddy, None if dX is None else dX.data_ptr(),
-                0 if dX is None else _TYPES[dX.dtype], lddx, dW.data_ptr(), _TYPES[dW.dtype], lddw,
-                _vector(db, "db", n, dev), M, k, n, self._ws(ws, self.workspace_bytes(M), dev), _base._stream(dev)))
+        _run(
+            L.mlp_dense_backward, dev, X.data_ptr(), ldx, W.data_ptr(), ldw, self.activation, None if stash is None else stash.data_ptr(),
+            dY.data_ptr(), _TYPES[dY.dtype], lddy, None if dX is None else dX.data_ptr(),
+            0 if dX is None else _TYPES[dX.dtype], lddx, dW.data_ptr(), _TYPES[dW.dtype], lddw,
+            _vector(db, "db", n, dev), M, k, n, self._ws(ws, self._ws_bytes(M), dev))
         return dX, dW, db
 
 
@@ -257,10 +270,10 @@ class SoftmaxHead(_Layer):
             if M == 0:
                 pH = pW  # an empty tensor has no address; nothing is written to it
         mode = _base.MLP_MODE_TRAIN if grads else _base.MLP_MODE_INFER
-        with torch.cuda.device(dev):
-            _base._check(fn(H.data_ptr(), ldh, W.data_ptr(), ldw, *args, loss.data_ptr(),
-                            _vector(row_loss, "row_loss", M, dev), pH, tH, lddh, pW, tW, lddw, M, d, v,
-                            self._ws(ws, self.workspace_bytes(M, mode, top), dev), _base._stream(dev)))
+        _run(
+            fn, dev, H.data_ptr(), ldh, W.data_ptr(), ldw, *args, loss.data_ptr(),
+            _vector(row_loss, "row_loss", M, dev), pH, tH, lddh, pW, tW, lddw, M, d, v,
+            self._ws(ws, self._ws_bytes(M, mode, top), dev))
         return (dH, dW, loss) if grads else loss
 
     def _target(self, target, ignore_index):
