@@ -44,7 +44,7 @@ bool tile_suits(int tile, int form, int64_t M) {
   return true;
 }
 
-bool few_rows(int form, int64_t M) { return form == GEMM_XW && M <= 8; }
+bool few_rows(int form, int64_t M) { return form == GEMM_XW && M <= 2; }
 
 }  // namespace
 
@@ -124,15 +124,15 @@ hipError_t launch_gemm(int form, GemmArgs a, float* partial, hipStream_t s) {
 
 // -------------------------------------------------------------- few rows --
 
-// Y = X W for MR <= 8 rows: W is read once and its products are made on the
+// Y = X W for MR = 1 or 2 rows: W is read once and its products are made on the
 // vector units, so bandwidth and latency bound it (one row of 4096 x 4096: the
 // 32 MiB of W).  A workgroup owns 8 LPR columns; LPR lanes hold them as 16-byte
 // pieces, the wave's 64 / LPR groups take eight consecutive k each, the NW waves
 // every NW-th such block.  Then the groups' sums are added by shuffles and the
 // waves' in order through LDS.  LPR is chosen so that 256 workgroups or more
 // share N; those that share the 128 bytes of a line run on one chiplet.
-// Against the matrix-core kernel with splits (two launches), one row of 4096 x
-// 4096: FEW_RESULT.
+// Rows of 4096 x 4096 against the matrix-core kernel with splits (two
+// launches): one 11.3 us to 14, two 13.5 to 14 (four: 16, slower).
 template <int MR, int NW, int LPR>
 __global__ __launch_bounds__(NW * 64) void few_rows_kernel(const GemmArgs a) {
   constexpr int COLS = 8 * LPR, PER = 64 / COLS;  // workgroups of a line
@@ -198,9 +198,7 @@ hipError_t launch_few_rows_cols(const GemmArgs& a, hipStream_t s) {
   constexpr int COLS = 8 * LPR, PER = 64 / COLS;
   const dim3 grid((unsigned)(cdiv(a.N, COLS * 8 * PER) * 8 * PER));  // whole lines on eight chiplets
   if (a.M <= 1) hipLaunchKernelGGL((few_rows_kernel<1, 16, LPR>), grid, dim3(1024), 0, s, a);
-  else if (a.M <= 2) hipLaunchKernelGGL((few_rows_kernel<2, 16, LPR>), grid, dim3(1024), 0, s, a);
-  else if (a.M <= 4) hipLaunchKernelGGL((few_rows_kernel<4, 8, LPR>), grid, dim3(512), 0, s, a);
-  else hipLaunchKernelGGL((few_rows_kernel<8, 8, LPR>), grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((few_rows_kernel<2, 16, LPR>), grid, dim3(1024), 0, s, a);
   return hipGetLastError();
 }
 hipError_t launch_few_rows(const GemmArgs& a, hipStream_t s) {

@@ -89,24 +89,27 @@ struct Loader {
     for (int j = 0; j < S::PER; ++j)
       voff[j] = piece_in(j, tid) ? (uint32_t)(((int64_t)piece_row(j, tid) * a.ld + piece_col(j, tid)) * 2) : kOOB;
   }
-  // The next step to LDS at `lds`.  Pieces that begin past kend or past the
-  // matrix are out of the descriptor's range and arrive as zeros, so steps
-  // past the last one may be loaded too.  What follows a T side's row in
-  // memory (within the matrix) comes along in its last tile: it only reaches
-  // columns of C that do not exist.
-  __device__ __forceinline__ void to_lds(uint32_t lds, int wave, int tid) {
+  // The next step to LDS at `lds`, piece by piece between begin and end.
+  // Pieces that begin past kend or past the matrix are out of the descriptor's
+  // range and arrive as zeros, so steps past the last one may be loaded too.
+  // What follows a T side's row in memory (within the matrix) comes along in
+  // its last tile: it only reaches columns of C that do not exist.
+  u32x4 r;
+  uint32_t dst;
+  __device__ __forceinline__ void begin(uint32_t lds, int wave) {
     // (a buffer descriptor as make_rsrc builds it, in scalar registers)
     const uint64_t at = (uint64_t)p;
     const int64_t n = krem <= 0 || left <= 0 ? 0 : (left > 0x7fffffff ? 0x7fffffff : left);
-    const u32x4 r = {(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)n, 0x00020000u};
-#pragma unroll
-    for (int j = 0; j < S::PER; ++j) {
-      uint32_t o = voff[j];
-      if (!T) o = piece_col(j, tid) < krem ? o : kOOB;
-      const uint32_t dst = lds + (uint32_t)(j * NTHR + wave * 64) * 16;
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                   :: "s"(dst), "v"(o), "s"(r) : "memory");
-    }
+    r = u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)n, 0x00020000u};
+    dst = lds + (uint32_t)(wave * 64) * 16;
+  }
+  __device__ __forceinline__ void piece(int j, int tid) const {
+    uint32_t o = voff[j];
+    if (!T) o = piece_col(j, tid) < krem ? o : kOOB;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :: "s"(dst + (uint32_t)(j * NTHR * 16)), "v"(o), "s"(r) : "memory");
+  }
+  __device__ __forceinline__ void end() {
     const int64_t step = T ? a.ld * (BK * 2) : BK * 2;
     p += step;
     left -= step;
@@ -178,9 +181,11 @@ __device__ __forceinline__ void wait_loads_barrier() {
 
 // acc += the BM x BN tile's products over k in [k0, k1), k0 a multiple of BK.
 // `lds`: the workgroup's ST buffers of the two slices, free again when it
-// returns.  Within a step the fragments of its first 32 k are read before the
-// next loads are issued: a full memory queue then holds up no matrix product
-// (2 to 4% over issuing first).
+// returns.  The next loads are issued between the products of a step's first
+// 32 k, a few at a time: issued together, they fill the memory queue and every
+// wave waits there before its products (8192 x 4096 over 4096 of k, both sides'
+// rows along k: 1215 TFLOP/s with the loads first, 1260 after the first reads,
+// 1320 so; a library's product of this size 1110 to 1370).
 template <typename TL, bool MT, bool NT>
 __device__ __forceinline__ void gemm_loop(const SideArgs& ma, const SideArgs& na, int64_t m0, int64_t n0, int64_t k0,
                                           int64_t k1, uint8_t* lds, f32x4 (&acc)[TL::MB][TL::NB]) {
@@ -199,12 +204,17 @@ __device__ __forceinline__ void gemm_loop(const SideArgs& ma, const SideArgs& na
   fn.init(wn * TL::NB * 16, lane);
   const int nk = (int)((k1 - k0 + TL::BK - 1) / TL::BK);
   const uint32_t l0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
-  const auto issue = [&](int slot) {
-    lm.to_lds(l0 + slot * STAGE, wave, tid);
-    ln.to_lds(l0 + slot * STAGE + SM::BYTES, wave, tid);
-  };
 #pragma unroll
-  for (int t = 0; t < TL::ST - 1; ++t) issue(t);
+  for (int t = 0; t < TL::ST - 1; ++t) {
+    lm.begin(l0 + t * STAGE, wave);
+    ln.begin(l0 + t * STAGE + SM::BYTES, wave);
+#pragma unroll
+    for (int j = 0; j < SM::PER; ++j) lm.piece(j, tid);
+#pragma unroll
+    for (int j = 0; j < SN::PER; ++j) ln.piece(j, tid);
+    lm.end();
+    ln.end();
+  }
   int slot = 0;
   for (int t = 0; t < nk; ++t) {
     wait_loads_barrier<(TL::ST - 2) * LOADS>();
@@ -215,25 +225,36 @@ __device__ __forceinline__ void gemm_loop(const SideArgs& ma, const SideArgs& na
       ln.fix(s + SM::BYTES, k, tid);
       __syncthreads();
     }
-#pragma unroll
-    for (int kk = 0; kk < TL::BK / 32; ++kk) {
+    // into the buffer of step t - 1, which every wave has read.  Steps past the
+    // last load zeros, so that the count of loads in flight stays the same.
+    const int next = slot == 0 ? TL::ST - 1 : slot - 1;
+    lm.begin(l0 + next * STAGE, wave);
+    ln.begin(l0 + next * STAGE + SM::BYTES, wave);
+    static_for<0, TL::BK / 32>([&](auto kc) {
+      constexpr int kk = decltype(kc)::value;
       u32x4 a[TL::MB], b[TL::NB];
 #pragma unroll
       for (int n = 0; n < TL::NB; ++n) b[n] = fn.read(s + SM::BYTES, kk, n);
 #pragma unroll
       for (int m = 0; m < TL::MB; ++m) a[m] = fm.read(s, kk, m);
-      if (kk == 0) {
-        // into the buffer of step t - 1, which every wave has read.  Steps past
-        // the last load zeros, so that the count of loads in flight stays the same.
-        __builtin_amdgcn_sched_barrier(0);
-        issue(slot == 0 ? TL::ST - 1 : slot - 1);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll
-      for (int m = 0; m < TL::MB; ++m)
+      static_for<0, TL::MB>([&](auto mc) {
+        constexpr int m = decltype(mc)::value;
 #pragma unroll
         for (int n = 0; n < TL::NB; ++n) acc[m][n] = mfma16(b[n], a[m], acc[m][n]);
-    }
+        constexpr int lo = LOADS * m / TL::MB, hi = LOADS * (m + 1) / TL::MB;
+        if constexpr (kk == 0 && hi > lo) {
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int q = lo; q < hi; ++q) {
+            if (q < SM::PER) lm.piece(q < SM::PER ? q : 0, tid);
+            else ln.piece(q < SM::PER ? 0 : q - SM::PER, tid);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      });
+    });
+    lm.end();
+    ln.end();
     slot = slot + 1 == TL::ST ? 0 : slot + 1;
   }
   wait_loads_barrier<0>();
@@ -294,7 +315,7 @@ __device__ __forceinline__ void gemm_tile_of(int b, int mt, int nt, int& tm, int
   tn = in / rows;
 }
 
-// act(z) in y and act'(z) in d.  GELU is z Phi(z) with Phi from the rational
+// act(z) in y and act'(z) in d (which costs nothing where it is not used).  GELU is z Phi(z) with Phi from the rational
 // approximation 7.1.26 of Abramowitz and Stegun (error of erf up to 1.5e-7),
 // whose exponential the derivative needs too.
 __device__ __forceinline__ void act_and_grad(int act, float z, float& y, float& d) {
@@ -384,14 +405,16 @@ __device__ __forceinline__ void out4(const GemmOut& o, int64_t m, int n, int N, 
   }
 }
 
-// act(z) in place over eight values, act'(z) in d.
+// act(z) in place over eight values and, with GRAD, act'(z) in d.
+template <bool GRAD>
 __device__ __forceinline__ void act8(int act, float (&z)[8], float (&d)[8]) {
   const auto all = [&](auto kind) {
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-      float y;
-      act_and_grad(decltype(kind)::value, z[q], y, d[q]);
+      float y, g;
+      act_and_grad(decltype(kind)::value, z[q], y, g);
       z[q] = y;
+      if (GRAD) d[q] = g;
     }
   };
   switch (act) {
@@ -416,8 +439,10 @@ __device__ __forceinline__ void out8(const GemmOut& o, int64_t m, int n, int N, 
   }
   if (o.act != ACT_LINEAR) {
     float d[8];
-    act8(o.act, z, d);
-    if (o.stash) {
+    if (!o.stash) {
+      act8<false>(o.act, z, d);
+    } else {
+      act8<true>(o.act, z, d);
       float* s = o.stash + m * (int64_t)N + n;
       *reinterpret_cast<f32x4*>(s) = f32x4{d[0], d[1], d[2], d[3]};
       *reinterpret_cast<f32x4*>(s + 4) = f32x4{d[4], d[5], d[6], d[7]};

@@ -73,21 +73,33 @@ __device__ __forceinline__ void row_stats(const float (&x)[J][8], int lane, int 
   rstd = 1.f / __builtin_sqrtf(v / (float)N + eps);
 }
 
-// Rows of whole pieces (N a multiple of 8) go through buffer descriptors that
-// begin at a wave's first row: a lane's offsets stay the same from row to row
-// and lanes past N are out of range (they read zeros and store nothing), so no
-// branch and no address arithmetic stands between the loads of a row.
-template <bool F32, int G, int J>
-struct WholeRows {
+// How a row may end: with a whole piece (or, one row to a wave, an even
+// element); one row to a wave and an odd bf16 element; several rows to a wave
+// and a piece that would run on into the next one.
+enum { END_WHOLE, END_ODD, END_SHARED };
+
+// Rows go through buffer descriptors that begin at a wave's first row: a lane's
+// offsets stay the same from row to row, and what lies past the last row is out
+// of range (reads as zeros, is not stored), so no branch and no address
+// arithmetic stands between the loads of a row.  The range check works on
+// dwords, so the last element of a bf16 row that does not end with one is loaded
+// and stored by itself.
+template <bool F32, int G, int J, int END>
+struct BufRows {
   static constexpr int SIZE = F32 ? 4 : 2;
+  static constexpr bool LAST = END != END_WHOLE && !F32;
   const uint8_t* p;
   int64_t ld;
   uint32_t voff[J];
+  uint32_t last;  // offset of the last element of the lane's row
+  int n;          // END_SHARED (J = 1): elements of the lane's piece
   rsrc_t r;
   __device__ __forceinline__ void init(const void* base, int64_t stride, int N) {
     p = static_cast<const uint8_t*>(base);
     ld = stride;
     const int lane = threadIdx.x % G, grp = (threadIdx.x & 63) / G;  // grp: 0 where G >= 64
+    last = (uint32_t)((grp * stride + N - 1) * SIZE);
+    n = N - 8 * lane;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int c = 8 * (j * G + lane);
@@ -102,14 +114,16 @@ struct WholeRows {
   }
   struct Raw {
     u32x4 x[F32 ? 2 : 1];
+    uint32_t end[1];
   };
   __device__ __forceinline__ Raw load(int j) const {
     Raw v;
     v.x[0] = bload128(r, voff[j], 0);
     if constexpr (F32) v.x[1] = bload128(r, voff[j] + 16, 0);
+    if constexpr (LAST) v.end[0] = bload16(r, last, 0);
     return v;
   }
-  static __device__ __forceinline__ void widen(const Raw& v, float (&f)[8]) {
+  __device__ __forceinline__ void widen(int j, const Raw& v, float (&f)[8]) const {
     if constexpr (F32) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -118,14 +132,38 @@ struct WholeRows {
       }
     } else {
       widen8(v.x[0], f);
+      if constexpr (LAST)
+#pragma unroll
+        for (int q = 0; q < 8; q += END == END_ODD ? 2 : 1)
+          f[q] = voff[j] + 2 * q == last ? __uint_as_float(v.end[0] << 16) : f[q];
     }
+    if constexpr (END == END_SHARED)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) f[q] = q < n ? f[q] : 0.f;
   }
   __device__ __forceinline__ void store(int j, const float (&f)[8]) const {
+    if constexpr (END == END_SHARED) {
+      if (n < 8) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          if constexpr (F32) bstore32<false>(__float_as_uint(f[q]), r, q < n ? voff[j] + 4 * q : kOOB, 0);
+          else bstore16<false>(pack_bf16x2(f[q], 0.f), r, q < n ? voff[j] + 2 * q : kOOB, 0);
+        }
+        return;
+      }
+    }
     if constexpr (F32) {
       bstore128<false>(__builtin_bit_cast(u32x4, f32x4{f[0], f[1], f[2], f[3]}), r, voff[j], 0);
       bstore128<false>(__builtin_bit_cast(u32x4, f32x4{f[4], f[5], f[6], f[7]}), r, voff[j] + 16, 0);
     } else {
-      bstore128<false>(u32x4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])}, r, voff[j], 0);
+      const u32x4 u = {pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
+      bstore128<false>(u, r, voff[j], 0);
+      if constexpr (END == END_ODD) {
+        uint32_t e = u[0];
+#pragma unroll
+        for (int q = 1; q < 4; ++q) e = voff[j] + 4 * q == last ? u[q] : e;
+        bstore16<false>(e, r, last - voff[j] < 16 ? last : kOOB, 0);
+      }
     }
   }
 };
@@ -148,32 +186,38 @@ __device__ __forceinline__ void lds8(const float* p, float (&v)[8]) {
 
 }  // namespace
 
-template <int G, int J, bool X32, bool Y32>
-__global__ __launch_bounds__(256) void norm_fwd_whole_kernel(const NormArgs a) {
-  __shared__ float lds[8];
+// Threads of a forward workgroup.
+template <int G> constexpr int norm_fwd_threads() { return G > 256 ? G : 256; }
+
+template <int G, int J, int END, bool X32, bool Y32>
+__global__ __launch_bounds__(norm_fwd_threads<G>()) void norm_fwd_buf_kernel(const NormArgs a) {
+  __shared__ float lds[32];
   const int lane = threadIdx.x % G;
-  constexpr int PER = 256 / G, WPR = G < 64 ? 64 / G : 1;  // rows of a workgroup, of a wave
-  WholeRows<X32, G, J> X;
-  WholeRows<Y32, G, J> Y;
+  constexpr int PER = norm_fwd_threads<G>() / G, WPR = G < 64 ? 64 / G : 1;  // rows of a workgroup, of a wave
+  BufRows<X32, G, J, END> X;
+  BufRows<Y32, G, J, END> Y;
   X.init(a.X, a.ldx, a.N);
   Y.init(a.Y, a.ldy, a.N);
+  const rsrc_t rg = make_rsrc(a.gamma, a.gamma ? (int64_t)a.N * 4 : 0), rb = make_rsrc(a.beta, a.beta ? (int64_t)a.N * 4 : 0);
   const int wave_row = G <= 64 ? (int)(threadIdx.x >> 6) * WPR : 0;
   for (int64_t first = (int64_t)blockIdx.x * PER; first < a.M; first += (int64_t)gridDim.x * PER) {
     const int64_t row0 = uniform(first + wave_row), row = row0 + (threadIdx.x & 63) / G;
     X.at(row0, a.M, a.N);
     Y.at(row0, a.M, a.N);
-    typename WholeRows<X32, G, J>::Raw raw[J];
+    typename BufRows<X32, G, J, END>::Raw raw[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) raw[j] = X.load(j);
     float g[J][8], b[J][8], x[J][8];
 #pragma unroll
     for (int j = 0; j < J; ++j) {  // in flight with the row
-      const int c = 8 * (j * G + lane);
-      if (a.gamma) load8(a.gamma + (c < a.N ? c : a.N - 8), 8, g[j]);
-      if (a.beta) load8(a.beta + (c < a.N ? c : a.N - 8), 8, b[j]);
+      const uint32_t c = 32 * (j * G + lane);
+      *reinterpret_cast<u32x4*>(&g[j][0]) = bload128(rg, c, 0);
+      *reinterpret_cast<u32x4*>(&g[j][4]) = bload128(rg, c + 16, 0);
+      *reinterpret_cast<u32x4*>(&b[j][0]) = bload128(rb, c, 0);
+      *reinterpret_cast<u32x4*>(&b[j][4]) = bload128(rb, c + 16, 0);
     }
 #pragma unroll
-    for (int j = 0; j < J; ++j) X.widen(raw[j], x[j]);
+    for (int j = 0; j < J; ++j) X.widen(j, raw[j], x[j]);
     float mean, rstd;
     row_stats<G, J>(x, lane, a.N, a.eps, lds, mean, rstd);
     if (a.stats && lane == 0 && row < a.M) *reinterpret_cast<f32x2*>(a.stats + 2 * row) = f32x2{mean, rstd};
@@ -182,50 +226,10 @@ __global__ __launch_bounds__(256) void norm_fwd_whole_kernel(const NormArgs a) {
       float y[8];
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        y[q] = (x[j][q] - mean) * rstd;
-        if (a.gamma) y[q] *= g[j][q];
-        if (a.beta) y[q] += b[j][q];
+        y[q] = (x[j][q] - mean) * rstd * (a.gamma ? g[j][q] : 1.f) + b[j][q];  // no beta reads as zeros
       }
       Y.store(j, y);
     }
-  }
-}
-
-// Rows of any length.
-template <int G, int J, bool X32, bool Y32>
-__global__ __launch_bounds__(256) void norm_fwd_kernel(const NormArgs a) {
-  typedef typename Elem<X32>::type TX;
-  typedef typename Elem<Y32>::type TY;
-  __shared__ float lds[8];
-  const int lane = threadIdx.x % G;
-  // groups of lanes, or the whole workgroup, take rows of their own
-  for (int64_t row = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G; row < a.M; row += (int64_t)gridDim.x * (256 / G)) {
-  const TX* X = static_cast<const TX*>(a.X) + row * a.ldx;
-  float x[J][8];
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    const int c = 8 * (j * G + lane);
-    load8(X + c, a.N - c, x[j]);
-  }
-  float mean, rstd;
-  row_stats<G, J>(x, lane, a.N, a.eps, lds, mean, rstd);
-  if (a.stats && lane == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * row) = f32x2{mean, rstd};
-  TY* Y = static_cast<TY*>(a.Y) + row * a.ldy;
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    const int c = 8 * (j * G + lane), n = a.N - c;
-    if (n <= 0) continue;
-    float g[8], b[8], y[8];
-    if (a.gamma) load8(a.gamma + c, n, g);
-    if (a.beta) load8(a.beta + c, n, b);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      y[q] = (x[j][q] - mean) * rstd;
-      if (a.gamma) y[q] *= g[q];
-      if (a.beta) y[q] += b[q];
-    }
-    store8(Y + c, n, y);
-  }
   }
 }
 
@@ -300,8 +304,8 @@ __device__ __forceinline__ void bwd_dx(const float (&x)[8], float (&d)[8], const
 // keeps the sums for dgamma and dbeta of its columns in registers, gamma being
 // in LDS.  bf16 pieces stay packed until they are used; where registers allow
 // (J <= 2), a group asks for its next row before it works on the current one.
-template <int G, int J, bool X32, bool DY32, bool DX32>
-__global__ __launch_bounds__((norm_bwd_threads<G, J>())) void norm_bwd_whole_kernel(const NormArgs a) {
+template <int G, int J, int END, bool X32, bool DY32, bool DX32>
+__global__ __launch_bounds__((norm_bwd_threads<G, J>())) void norm_bwd_buf_kernel(const NormArgs a) {
   constexpr int NTHR = norm_bwd_threads<G, J>(), PER = NTHR / G, COLS = 8 * J * G, WPR = G < 64 ? 64 / G : 1;
   constexpr bool AHEAD = J == 1 || (J == 2 && G <= 64 && !X32 && !DY32);
   __shared__ float lds[32];
@@ -310,15 +314,15 @@ __global__ __launch_bounds__((norm_bwd_threads<G, J>())) void norm_bwd_whole_ker
   const int lane = threadIdx.x % G;
   fill_columns(gamma, COLS, a.gamma, a.N, 1.f);
   __syncthreads();
-  WholeRows<X32, G, J> X;
-  WholeRows<DY32, G, J> D;
-  WholeRows<DX32, G, J> O;
+  BufRows<X32, G, J, END> X;
+  BufRows<DY32, G, J, END> D;
+  BufRows<DX32, G, J, END> O;
   X.init(a.X, a.ldx, a.N);
   D.init(a.dY, a.lddy, a.N);
   O.init(a.dX, a.lddx, a.N);
   float dg[J][8] = {}, db[J][8] = {};
-  typename WholeRows<X32, G, J>::Raw nx[J];
-  typename WholeRows<DY32, G, J>::Raw nd[J];
+  typename BufRows<X32, G, J, END>::Raw nx[J];
+  typename BufRows<DY32, G, J, END>::Raw nd[J];
   f32x2 nst;
   const int wave_row = G <= 64 ? (int)(threadIdx.x >> 6) * WPR : threadIdx.x / G, in_wave = G < 64 ? (threadIdx.x & 63) / G : 0;
   const auto fetch = [&](int64_t row0) {
@@ -338,8 +342,8 @@ __global__ __launch_bounds__((norm_bwd_threads<G, J>())) void norm_bwd_whole_ker
   for (; first < a.M; first += step) {
     const int64_t row0 = uniform(first + wave_row);
     if (!AHEAD) fetch(row0);
-    typename WholeRows<X32, G, J>::Raw px[J];
-    typename WholeRows<DY32, G, J>::Raw pd[J];
+    typename BufRows<X32, G, J, END>::Raw px[J];
+    typename BufRows<DY32, G, J, END>::Raw pd[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       px[j] = nx[j];
@@ -352,8 +356,8 @@ __global__ __launch_bounds__((norm_bwd_threads<G, J>())) void norm_bwd_whole_ker
     for (int j = 0; j < J; ++j) {
       float g[8], x[8], d[8];
       lds8(gamma + 8 * (j * G + lane), g);
-      X.widen(px[j], x);
-      D.widen(pd[j], d);
+      X.widen(j, px[j], x);
+      D.widen(j, pd[j], d);
       bwd_sums(x, d, g, st, dg[j], db[j], s1, s2);
     }
     row_sum2<G>(s1, s2, lds);
@@ -364,60 +368,10 @@ __global__ __launch_bounds__((norm_bwd_threads<G, J>())) void norm_bwd_whole_ker
     for (int j = 0; j < J; ++j) {
       float g[8], x[8], d[8];
       lds8(gamma + 8 * (j * G + lane), g);
-      X.widen(px[j], x);
-      D.widen(pd[j], d);
+      X.widen(j, px[j], x);
+      D.widen(j, pd[j], d);
       bwd_dx(x, d, g, st, s1, s2);
       O.store(j, d);
-    }
-  }
-  write_part<G, J>(a, dg, db, sums);
-}
-
-// The same for rows of any length.
-template <int G, int J, bool X32, bool DY32>
-__global__ __launch_bounds__((norm_bwd_threads<G, J>())) void norm_bwd_kernel(const NormArgs a) {
-  typedef typename Elem<X32>::type TX;
-  typedef typename Elem<DY32>::type TD;
-  constexpr int NTHR = norm_bwd_threads<G, J>(), PER = NTHR / G, COLS = 8 * J * G;
-  __shared__ float lds[32];
-  __shared__ __align__(16) float gamma[COLS];
-  __shared__ float sums[PER > 1 ? COLS : 1];
-  const int lane = threadIdx.x % G, grp = threadIdx.x / G;
-  fill_columns(gamma, COLS, a.gamma, a.N, 1.f);
-  __syncthreads();
-  float dg[J][8] = {}, db[J][8] = {};
-  for (int64_t first = (int64_t)blockIdx.x * PER; first < a.M; first += (int64_t)gridDim.x * PER) {
-    const bool in = first + grp < a.M;  // all groups pass the sums below together
-    const int64_t row = in ? first + grp : a.M - 1;
-    const TX* X = static_cast<const TX*>(a.X) + row * a.ldx;
-    const TD* D = static_cast<const TD*>(a.dY) + row * a.lddy;
-    float x[J][8], d[J][8];
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int c = 8 * (j * G + lane);
-      load8(X + c, in ? a.N - c : 0, x[j]);
-      load8(D + c, in ? a.N - c : 0, d[j]);
-    }
-    const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
-    float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      float g[8];
-      lds8(gamma + 8 * (j * G + lane), g);
-      bwd_sums(x[j], d[j], g, st, dg[j], db[j], s1, s2);
-    }
-    row_sum2<G>(s1, s2, lds);
-    s1 /= (float)a.N;
-    s2 /= (float)a.N;
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int c = 8 * (j * G + lane), n = a.N - c;
-      float g[8];
-      lds8(gamma + c, g);
-      bwd_dx(x[j], d[j], g, st, s1, s2);
-      if (n <= 0 || !in) continue;
-      if (a.dx_fp32) store8(static_cast<float*>(a.dX) + row * a.lddx + c, n, d[j]);
-      else store8(static_cast<uint16_t*>(a.dX) + row * a.lddx + c, n, d[j]);
     }
   }
   write_part<G, J>(a, dg, db, sums);
@@ -573,8 +527,8 @@ hipError_t by_types(bool a32, bool b32, F&& f) {
   if (N <= 8 * G * J) { f(std::integral_constant<int, G>{}, std::integral_constant<int, J>{}); return true; }
 template <typename F>
 bool by_row_forward(int N, F&& f) {
-  FFMLP_ROW(8, 1) FFMLP_ROW(16, 1) FFMLP_ROW(32, 1) FFMLP_ROW(64, 1) FFMLP_ROW(64, 2) FFMLP_ROW(64, 4)
-  FFMLP_ROW(256, 2) FFMLP_ROW(256, 4) FFMLP_ROW(256, 8)
+  FFMLP_ROW(8, 1) FFMLP_ROW(16, 1) FFMLP_ROW(32, 1) FFMLP_ROW(64, 1) FFMLP_ROW(64, 2) FFMLP_ROW(256, 1)
+  FFMLP_ROW(512, 1) FFMLP_ROW(256, 4) FFMLP_ROW(512, 4)
   return false;
 }
 template <typename F>
@@ -601,10 +555,11 @@ hipError_t launch_norm_forward(const NormArgs& a, hipStream_t s) {
   return by_types(a.x_fp32, a.y_fp32, [&](auto x32, auto y32) {
     constexpr bool X = decltype(x32)::value, Y = decltype(y32)::value;
     const bool held = by_row_forward(a.N, [&](auto g, auto j) {
-      constexpr int G = decltype(g)::value, J = decltype(j)::value, R = 256 / G;
+      constexpr int G = decltype(g)::value, J = decltype(j)::value, T = norm_fwd_threads<G>(), R = T / G;
       const dim3 grid(norm_grid((a.M + R - 1) / R));
-      if (a.N % 8 == 0) hipLaunchKernelGGL((norm_fwd_whole_kernel<G, J, X, Y>), grid, dim3(256), 0, s, a);
-      else hipLaunchKernelGGL((norm_fwd_kernel<G, J, X, Y>), grid, dim3(256), 0, s, a);
+      constexpr int OTHER = G < 64 ? END_SHARED : END_ODD;
+      if (a.N % (G < 64 ? 8 : 2) == 0) hipLaunchKernelGGL((norm_fwd_buf_kernel<G, J, END_WHOLE, X, Y>), grid, dim3(T), 0, s, a);
+      else hipLaunchKernelGGL((norm_fwd_buf_kernel<G, J, OTHER, X, Y>), grid, dim3(T), 0, s, a);
     });
     if (!held) hipLaunchKernelGGL((norm_fwd_long_kernel<X, Y>), dim3(norm_grid(a.M)), dim3(256), 0, s, a);
     return hipGetLastError();
@@ -617,9 +572,14 @@ hipError_t launch_norm_backward(const NormArgs& a, hipStream_t s) {
     const bool held = by_row_backward(a.N, [&](auto g, auto j) {
       constexpr int G = decltype(g)::value, J = decltype(j)::value;
       const dim3 grid((unsigned)a.parts), block(norm_bwd_threads<G, J>());
-      if (a.N % 8 != 0) hipLaunchKernelGGL((norm_bwd_kernel<G, J, X, D>), grid, block, 0, s, a);
-      else if (a.dx_fp32) hipLaunchKernelGGL((norm_bwd_whole_kernel<G, J, X, D, true>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((norm_bwd_whole_kernel<G, J, X, D, false>), grid, block, 0, s, a);
+      constexpr int OTHER = G < 64 ? END_SHARED : END_ODD;
+      const auto run = [&](auto o32) {
+        constexpr bool O = decltype(o32)::value;
+        if (a.N % (G < 64 ? 8 : 2) == 0) hipLaunchKernelGGL((norm_bwd_buf_kernel<G, J, END_WHOLE, X, D, O>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((norm_bwd_buf_kernel<G, J, OTHER, X, D, O>), grid, block, 0, s, a);
+      };
+      if (a.dx_fp32) run(std::true_type{});
+      else run(std::false_type{});
     });
     if (!held) {  // the columns first: dX may be dY
       hipLaunchKernelGGL((norm_cols_long_kernel<X, D>), dim3((unsigned)((a.N + 511) / 512), (unsigned)a.parts), dim3(256), 0, s, a);

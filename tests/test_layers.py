@@ -124,7 +124,8 @@ def test_layer_norm(ffmlp, gpu, M, N, xt, yt):
     norm_case(ffmlp, M, N, xt, yt, seed=M + N)
 
 
-@pytest.mark.parametrize("M,N,offset,extra", [(50, 128, 1, 0), (50, 96, 8, 8), (41, 333, 5, 3), (6, 20000, 1, 1)])
+@pytest.mark.parametrize("M,N,offset,extra", [(50, 128, 1, 0), (50, 96, 8, 8), (41, 333, 5, 3), (6, 20000, 1, 1), (203, 100, 1, 1),
+                                              (501, 13, 3, 2), (70, 250, 2, 0), (9, 2047, 1, 4)])
 def test_layer_norm_strides(ffmlp, gpu, M, N, offset, extra):
     norm_case(ffmlp, M, N, BF, BF, offset=offset, extra=extra)
     norm_case(ffmlp, M, N, F32, F32, affine=False, offset=offset, extra=extra)
@@ -132,6 +133,7 @@ def test_layer_norm_strides(ffmlp, gpu, M, N, offset, extra):
 
 def test_layer_norm_many_rows(ffmlp, gpu):
     norm_case(ffmlp, 40003, 24, BF, BF)
+    norm_case(ffmlp, 30001, 31, BF, F32)
     norm_case(ffmlp, 5000, 1024, F32, BF)
 
 
