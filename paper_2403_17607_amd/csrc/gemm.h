@@ -27,8 +27,6 @@ struct GemmOut {
   void* C;             // [M][ldc], bf16 or fp32
   int64_t ldc;
   int c_fp32;
-  int vec;             // every row of C, R, add and stash allows accesses of four columns,
-  int vec8;            // and N is a multiple of 8 and they allow 16-byte accesses of them
 };
 
 struct GemmArgs {

@@ -44,13 +44,13 @@ bool tile_suits(int tile, int form, int64_t M) {
   return true;
 }
 
-bool few_rows(int form, int64_t M) { return form == GEMM_XW && M <= 2; }
+bool one_row(int form, int64_t M) { return form == GEMM_XW && M == 1; }
 
 }  // namespace
 
 GemmPlan gemm_plan(int form, int64_t M, int64_t N, int64_t K) {
   GemmPlan best{};
-  if (few_rows(form, M)) return best;
+  if (one_row(form, M)) return best;
   double best_us = 0;
   for (const TileCost& t : kTiles) {
     if (!tile_suits(t.tile, form, M)) continue;
@@ -74,38 +74,41 @@ GemmPlan gemm_plan(int form, int64_t M, int64_t N, int64_t K) {
   return best;
 }
 
-// The splits' partial sums added in order, then the epilogue.
+// The splits' partial sums added in order, then the epilogue; a thread has eight
+// columns of a row.
 __global__ __launch_bounds__(256) void split_sum_kernel(const float* partial, int splits, int64_t M, int N, const GemmOut o) {
-  const int per = (N + 3) / 4;
+  const int per = (N + 7) / 8;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= M * per) return;
   const int64_t m = i / per;
-  const int n = (int)(i % per) * 4;
+  const int n = (int)(i % per) * 8;
   const float* p = partial + m * N + n;
-  f32x4 z = {0.f, 0.f, 0.f, 0.f};
-  if ((N & 3) == 0) {
-    int s = 0;
-    for (; s + 4 <= splits; s += 4, p += 4 * M * N) {  // four loads in flight, added in order
-      f32x4 v[4];
+  float z[8] = {}, b[8];
+  bias8(o, n, N, b);
+  int s = 0;
+  for (; s + 4 <= splits; s += 4, p += 4 * M * N) {  // four loads in flight, added in order
+    float v[4][8];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const f32x4*>(p + k * M * N);
+    for (int k = 0; k < 4; ++k) load8(p + k * M * N, N - n, v[k]);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) z += v[k];
-    }
-    for (; s < splits; ++s, p += M * N) z += *reinterpret_cast<const f32x4*>(p);
-  } else {
-    for (int s = 0; s < splits; ++s, p += M * N)
+    for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) z[q] += n + q < N ? p[q] : 0.f;
+      for (int q = 0; q < 8; ++q) z[q] += v[k][q];
   }
-  out4(o, m, n, N, z);
+  for (; s < splits; ++s, p += M * N) {
+    float v[8];
+    load8(p, N - n, v);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) z[q] += v[q];
+  }
+  out8(o, m, n, N, z, b, o.alpha ? *o.alpha : 1.f);
 }
 
-hipError_t launch_few_rows(const GemmArgs& a, hipStream_t s);
+hipError_t launch_one_row(const GemmArgs& a, hipStream_t s);
 
 hipError_t launch_gemm(int form, GemmArgs a, float* partial, hipStream_t s) {
   if (a.M <= 0 || a.N <= 0) return hipSuccess;
-  if (few_rows(form, a.M)) return launch_few_rows(a, s);
+  if (one_row(form, a.M)) return launch_one_row(a, s);
   const GemmPlan p = gemm_plan(form, a.M, a.N, a.K);
   a.mt = p.mt;
   a.nt = p.nt;
@@ -113,40 +116,40 @@ hipError_t launch_gemm(int form, GemmArgs a, float* partial, hipStream_t s) {
   a.splits = p.splits;
   a.kper = p.kper;
   a.partial = partial;
-  hipError_t e = form == GEMM_XW   ? launch_gemm_xw(p.tile, a, s)
-                 : form == GEMM_DX ? launch_gemm_dx(p.tile, a, s)
-                                   : launch_gemm_dw(p.tile, a, s);
+  const hipError_t e = form == GEMM_XW   ? launch_gemm_xw(p.tile, a, s)
+                       : form == GEMM_DX ? launch_gemm_dx(p.tile, a, s)
+                                         : launch_gemm_dw(p.tile, a, s);
   if (e != hipSuccess || p.splits <= 1) return e;
-  const int64_t n = a.M * ((a.N + 3) / 4);
+  const int64_t n = a.M * ((a.N + 7) / 8);
   hipLaunchKernelGGL(split_sum_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, partial, p.splits, a.M, a.N, a.out);
   return hipGetLastError();
 }
 
-// -------------------------------------------------------------- few rows --
+// --------------------------------------------------------------- one row --
 
-// Y = X W for MR = 1 or 2 rows: W is read once and its products are made on the
-// vector units, so bandwidth and latency bound it (one row of 4096 x 4096: the
-// 32 MiB of W).  A workgroup owns 8 LPR columns; LPR lanes hold them as 16-byte
-// pieces, the wave's 64 / LPR groups take eight consecutive k each, the NW waves
-// every NW-th such block.  Then the groups' sums are added by shuffles and the
-// waves' in order through LDS.  LPR is chosen so that 256 workgroups or more
-// share N; those that share the 128 bytes of a line run on one chiplet.
-// Rows of 4096 x 4096 against the matrix-core kernel with splits (two
-// launches): one 11.3 us to 14, two 13.5 to 14 (four: 16, slower).
-template <int MR, int NW, int LPR>
-__global__ __launch_bounds__(NW * 64) void few_rows_kernel(const GemmArgs a) {
-  constexpr int COLS = 8 * LPR, PER = 64 / COLS;  // workgroups of a line
-  __shared__ float sums[NW][MR][COLS];
+// Y = X W for one row: W is read once and its products are made on the vector
+// units, so bandwidth and latency bound it (4096 x 4096: the 32 MiB of W, 6.5 us
+// at the rate of a large copy).  A workgroup owns 8 LPR columns; LPR lanes hold
+// them as 16-byte pieces, the wave's 64 / LPR groups take eight consecutive k
+// each, the 16 waves every 16th such block.  Then the groups' sums are added by
+// shuffles and the waves' in order through LDS.  LPR is chosen so that 256
+// workgroups or more share N; those that share the 128 bytes of a line run on
+// one chiplet.  4096 x 4096 with GELU: 11.3 us, against 13 of the matrix-core
+// kernel with splits (two launches), which two rows take too.
+template <int LPR>
+__global__ __launch_bounds__(1024) void one_row_kernel(const GemmArgs a) {
+  constexpr int COLS = 8 * LPR, PER = 64 / COLS, NW = 16;  // PER: workgroups of a line
+  __shared__ __align__(16) float sums[NW][COLS];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   // workgroup b runs on chiplet b % 8: its neighbour there is b + 8
   const int b = blockIdx.x, at = (b / (8 * PER) * 8 + b % 8) * PER + b / 8 % PER;
   const int n = at * COLS + 8 * (lane % LPR);
   const int cols = a.N - n;  // of this lane
-  float acc[MR][8] = {};
+  float acc[8] = {};
   if (cols > 0) {
     for (int64_t k = (wave * (64 / LPR) + lane / LPR) * 8; k < a.K; k += NW * (64 / LPR) * 8) {
       const int kn = a.K - k < 8 ? (int)(a.K - k) : 8;
-      u32x4 x[MR], w[8];
+      u32x4 w[8];
       if (cols >= 8 && kn == 8) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const u32x4_a2*>(a.n.p + (k + j) * a.n.ld + n);
@@ -154,55 +157,49 @@ __global__ __launch_bounds__(NW * 64) void few_rows_kernel(const GemmArgs a) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           w[j] = u32x4{0u, 0u, 0u, 0u};
-          if (j < kn)
-#pragma unroll
-            for (int q = 0; q < 8; ++q)
-              if (q < cols) w[j][q / 2] |= (uint32_t)a.n.p[(k + j) * a.n.ld + n + q] << (16 * (q & 1));
+          if (j < kn) w[j] = load8_bits(a.n.p + (k + j) * a.n.ld + n, cols);
         }
       }
-#pragma unroll
-      for (int m = 0; m < MR; ++m) x[m] = load8_bits(a.m.p + (m < a.M ? m : 0) * a.m.ld + k, kn);
+      float x[8];
+      load8(a.m.p + k, kn, x);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const float lo = bf16_lo(w[j][q]), hi = bf16_hi(w[j][q]);
-#pragma unroll
-          for (int m = 0; m < MR; ++m) {
-            const float v = j & 1 ? bf16_hi(x[m][j / 2]) : bf16_lo(x[m][j / 2]);
-            acc[m][2 * q] += v * lo;
-            acc[m][2 * q + 1] += v * hi;
-          }
+          acc[2 * q] += x[j] * bf16_lo(w[j][q]);
+          acc[2 * q + 1] += x[j] * bf16_hi(w[j][q]);
         }
     }
   }
 #pragma unroll
-  for (int m = 0; m < MR; ++m)
+  for (int q = 0; q < 8; ++q) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-#pragma unroll
-      for (int d = LPR; d < 64; d *= 2) acc[m][q] += __shfl_xor(acc[m][q], d);
-      if (lane < LPR) sums[wave][m][8 * lane + q] = acc[m][q];
-    }
+    for (int d = LPR; d < 64; d *= 2) acc[q] += __shfl_xor(acc[q], d);
+    if (lane < LPR) sums[wave][8 * lane + q] = acc[q];
+  }
   __syncthreads();
-  const int m = threadIdx.x / (COLS / 4), c = 4 * (threadIdx.x % (COLS / 4));
-  if (m >= MR || m >= a.M || at * COLS + c >= a.N) return;
-  f32x4 z = {0.f, 0.f, 0.f, 0.f};
+  const int c = at * COLS + 8 * threadIdx.x;
+  if (threadIdx.x >= LPR || c >= a.N) return;
+  float z[8] = {}, bias[8], v[8];
+  bias8(a.out, c, a.N, bias);
+#pragma unroll 4
+  for (int w = 0; w < NW; ++w) {
+    lds8(&sums[w][8 * threadIdx.x], v);
 #pragma unroll
-  for (int w = 0; w < NW; ++w) z += *reinterpret_cast<const f32x4*>(&sums[w][m][c]);
-  out4(a.out, m, at * COLS + c, a.N, z);
+    for (int q = 0; q < 8; ++q) z[q] += v[q];
+  }
+  out8(a.out, 0, c, a.N, z, bias, a.out.alpha ? *a.out.alpha : 1.f);
 }
 
 template <int LPR>
-hipError_t launch_few_rows_cols(const GemmArgs& a, hipStream_t s) {
+hipError_t launch_one_row_cols(const GemmArgs& a, hipStream_t s) {
   constexpr int COLS = 8 * LPR, PER = 64 / COLS;
-  const dim3 grid((unsigned)(cdiv(a.N, COLS * 8 * PER) * 8 * PER));  // whole lines on eight chiplets
-  if (a.M <= 1) hipLaunchKernelGGL((few_rows_kernel<1, 16, LPR>), grid, dim3(1024), 0, s, a);
-  else hipLaunchKernelGGL((few_rows_kernel<2, 16, LPR>), grid, dim3(1024), 0, s, a);
+  // whole lines on eight chiplets
+  hipLaunchKernelGGL((one_row_kernel<LPR>), dim3((unsigned)(cdiv(a.N, COLS * 8 * PER) * 8 * PER)), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
-hipError_t launch_few_rows(const GemmArgs& a, hipStream_t s) {
-  return a.N >= 64 * 256 ? launch_few_rows_cols<8>(a, s) : a.N >= 32 * 256 ? launch_few_rows_cols<4>(a, s) : launch_few_rows_cols<2>(a, s);
+hipError_t launch_one_row(const GemmArgs& a, hipStream_t s) {
+  return a.N >= 64 * 256 ? launch_one_row_cols<8>(a, s) : a.N >= 32 * 256 ? launch_one_row_cols<4>(a, s) : launch_one_row_cols<2>(a, s);
 }
 
 // ------------------------------------------------------------ column sums --

@@ -26,6 +26,7 @@
 
 #include "device.h"
 #include "gemm.h"
+#include "rows.h"
 
 namespace ffmlp {
 
@@ -275,15 +276,15 @@ constexpr int gemm_lds_bytes() {
   return loop > OutTile<TL>::BYTES ? loop : OutTile<TL>::BYTES;
 }
 
-// f(r, p): for each phase, rows r = 0 .. ROWS - 1 of the phase (this lane's),
-// p the lane's `WIDE` consecutive results of that row, columns WIDE (lane %
-// (COLS / WIDE)) on.  before(m): called before block m of acc is written.
-template <typename TL, int WIDE, typename B, typename F>
+// f(r, p) for rows r of the wave's: p the lane's eight consecutive results of
+// that row, columns 8 (lane % (COLS / 8)) on.  before(m): called before block m
+// of acc is written.
+template <typename TL, typename B, typename F>
 __device__ __forceinline__ void out_rows(uint8_t* lds, f32x4 (&acc)[TL::MB][TL::NB], B&& before, F&& f) {
   typedef OutTile<TL> O;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float* part = reinterpret_cast<float*>(lds) + wave * O::ROWS * O::LD;
-  constexpr int LPR = O::COLS / WIDE, RPI = 64 / LPR;
+  constexpr int LPR = O::COLS / 8, RPI = 64 / LPR;
   static_for<0, TL::MB / O::G>([&](auto pc) {
     constexpr int ph = decltype(pc)::value;
     static_for<0, O::G>([&](auto gc) {
@@ -295,7 +296,7 @@ __device__ __forceinline__ void out_rows(uint8_t* lds, f32x4 (&acc)[TL::MB][TL::
     });
     __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-    for (int r = lane / LPR; r < O::ROWS; r += RPI) f(ph * O::ROWS + r, part + r * O::LD + WIDE * (lane % LPR));
+    for (int r = lane / LPR; r < O::ROWS; r += RPI) f(ph * O::ROWS + r, part + r * O::LD + 8 * (lane % LPR));
     __builtin_amdgcn_wave_barrier();
   });
 }
@@ -341,70 +342,6 @@ __device__ __forceinline__ void act_and_grad(int act, float z, float& y, float& 
   }
 }
 
-// Four columns n .. n + 3 of row m of a product's result, as `o` says.
-__device__ __forceinline__ void out4(const GemmOut& o, int64_t m, int n, int N, f32x4 z) {
-  const bool vec = o.vec && n + 4 <= N;
-  if (o.add) {
-    const float* p = o.add + m * o.ldadd + n;
-    if (vec) z += *reinterpret_cast<const f32x4*>(p);
-    else
-#pragma unroll
-      for (int q = 0; q < 4; ++q) if (n + q < N) z[q] += p[q];
-  }
-  if (o.alpha) z *= *o.alpha;
-  if (o.bias) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) z[q] += o.bias[n + q < N ? n + q : N - 1];
-  }
-  if (o.act != ACT_LINEAR || o.stash) {
-    float d[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      float y;
-      act_and_grad(o.act, z[q], y, d[q]);
-      z[q] = y;
-    }
-    if (o.stash) {
-      float* p = o.stash + m * (int64_t)N + n;
-      if (vec) *reinterpret_cast<f32x4*>(p) = f32x4{d[0], d[1], d[2], d[3]};
-      else
-#pragma unroll
-        for (int q = 0; q < 4; ++q) if (n + q < N) p[q] = d[q];
-    }
-  }
-  if (o.c_fp32) {
-    float* p = static_cast<float*>(o.C) + m * o.ldc + n;
-    if (o.R) {
-      const float* r = static_cast<const float*>(o.R) + m * o.ldr + n;
-      if (vec) z += *reinterpret_cast<const f32x4*>(r);
-      else
-#pragma unroll
-        for (int q = 0; q < 4; ++q) if (n + q < N) z[q] += r[q];
-    }
-    if (vec) *reinterpret_cast<f32x4*>(p) = z;
-    else
-#pragma unroll
-      for (int q = 0; q < 4; ++q) if (n + q < N) p[q] = z[q];
-  } else {
-    uint16_t* p = static_cast<uint16_t*>(o.C) + m * o.ldc + n;
-    if (o.R) {
-      const uint16_t* r = static_cast<const uint16_t*>(o.R) + m * o.ldr + n;
-      if (vec) {
-        const u32x2 u = *reinterpret_cast<const u32x2*>(r);
-        z += f32x4{bf16_lo(u[0]), bf16_hi(u[0]), bf16_lo(u[1]), bf16_hi(u[1])};
-      } else {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) if (n + q < N) z[q] += __uint_as_float((uint32_t)r[q] << 16);
-      }
-    }
-    const u32x2 u = {pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])};
-    if (vec) *reinterpret_cast<u32x2*>(p) = u;
-    else
-#pragma unroll
-      for (int q = 0; q < 4; ++q) if (n + q < N) p[q] = (uint16_t)(u[q / 2] >> (16 * (q & 1)));
-  }
-}
-
 // act(z) in place over eight values and, with GRAD, act'(z) in d.
 template <bool GRAD>
 __device__ __forceinline__ void act8(int act, float (&z)[8], float (&d)[8]) {
@@ -427,48 +364,43 @@ __device__ __forceinline__ void act8(int act, float (&z)[8], float (&d)[8]) {
   }
 }
 
-// Eight columns n .. n + 7 of row m where o.vec8; b: the bias of these columns.
-__device__ __forceinline__ void out8(const GemmOut& o, int64_t m, int n, int N, const float* p, const float (&b)[8], float alpha) {
-  float z[8];
+// The bias of columns n .. n + 7 (zeros past N).
+__device__ __forceinline__ void bias8(const GemmOut& o, int n, int N, float (&b)[8]) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    f32x4 v = *reinterpret_cast<const f32x4*>(p + 4 * h);
-    if (o.add) v += *reinterpret_cast<const f32x4*>(o.add + m * o.ldadd + n + 4 * h);
+  for (int q = 0; q < 8; ++q) b[q] = 0.f;
+  if (o.bias && n < N) load8(o.bias + n, N - n, b);
+}
+
+// Columns n .. n + 7 of row m of a product's result (fewer where N ends), as `o`
+// says: z the sums, b the bias of these columns.  Rows may start at any element;
+// 16-byte accesses do (rows.h).
+__device__ __forceinline__ void out8(const GemmOut& o, int64_t m, int n, int N, float (&z)[8], const float (&b)[8], float alpha) {
+  const int left = N - n;
+  float v[8];
+  if (o.add) {
+    load8(o.add + m * o.ldadd + n, left, v);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) z[4 * h + q] = v[q] * alpha + b[4 * h + q];
+    for (int q = 0; q < 8; ++q) z[q] += v[q];
   }
+#pragma unroll
+  for (int q = 0; q < 8; ++q) z[q] = z[q] * alpha + b[q];
   if (o.act != ACT_LINEAR) {
     float d[8];
     if (!o.stash) {
       act8<false>(o.act, z, d);
     } else {
       act8<true>(o.act, z, d);
-      float* s = o.stash + m * (int64_t)N + n;
-      *reinterpret_cast<f32x4*>(s) = f32x4{d[0], d[1], d[2], d[3]};
-      *reinterpret_cast<f32x4*>(s + 4) = f32x4{d[4], d[5], d[6], d[7]};
+      store8(o.stash + m * (int64_t)N + n, left, d);
     }
   }
-  if (o.c_fp32) {
-    float* c = static_cast<float*>(o.C) + m * o.ldc + n;
-    const float* r = static_cast<const float*>(o.R) + m * o.ldr + n;
+  if (o.R) {
+    if (o.c_fp32) load8(static_cast<const float*>(o.R) + m * o.ldr + n, left, v);
+    else load8(static_cast<const uint16_t*>(o.R) + m * o.ldr + n, left, v);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      f32x4 v = {z[4 * h], z[4 * h + 1], z[4 * h + 2], z[4 * h + 3]};
-      if (o.R) v += *reinterpret_cast<const f32x4*>(r + 4 * h);
-      *reinterpret_cast<f32x4*>(c + 4 * h) = v;
-    }
-  } else {
-    if (o.R) {
-      const u32x4 u = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(o.R) + m * o.ldr + n);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        z[2 * q] += bf16_lo(u[q]);
-        z[2 * q + 1] += bf16_hi(u[q]);
-      }
-    }
-    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(o.C) + m * o.ldc + n) =
-        u32x4{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3]), pack_bf16x2(z[4], z[5]), pack_bf16x2(z[6], z[7])};
+    for (int q = 0; q < 8; ++q) z[q] += v[q];
   }
+  if (o.c_fp32) store8(static_cast<float*>(o.C) + m * o.ldc + n, left, z);
+  else store8(static_cast<uint16_t*>(o.C) + m * o.ldc + n, left, z);
 }
 
 // C = the product, or one split's share of it as fp32 partial sums.
@@ -493,29 +425,21 @@ __global__ __launch_bounds__(TL::NTHR, 2) void gemm_kernel(const GemmArgs a) {
     o.C = a.partial + (int64_t)split * a.M * a.N;
     o.ldc = a.N;
     o.c_fp32 = 1;
-    o.vec = (a.N & 3) == 0;
-    o.vec8 = (a.N & 7) == 0;
   }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   constexpr int COLS = OutTile<TL>::COLS;
   const int64_t mw = m0 + (wave / TL::WN) * TL::MB * 16;
   const int nw = n0 + (wave % TL::WN) * COLS;
-  const auto none = [](auto) {};
-  if (o.vec8) {
-    const int n = nw + 8 * (lane % (COLS / 8));
-    const float alpha = o.alpha ? *o.alpha : 1.f;
-    float bias[8];
-#pragma unroll
-    for (int q = 0; q < 8; ++q) bias[q] = o.bias && n < a.N ? o.bias[n + q] : 0.f;
-    out_rows<TL, 8>(gemm_lds, acc, none, [&](int r, const float* p) {
-      if (mw + r < a.M && n < a.N) out8(o, mw + r, n, a.N, p, bias, alpha);
-    });
-  } else {
-    const int n = nw + 4 * (lane % (COLS / 4));
-    out_rows<TL, 4>(gemm_lds, acc, none, [&](int r, const float* p) {
-      if (mw + r < a.M && n < a.N) out4(o, mw + r, n, a.N, *reinterpret_cast<const f32x4*>(p));
-    });
-  }
+  const int n = nw + 8 * (lane % (COLS / 8));
+  const float alpha = o.alpha ? *o.alpha : 1.f;
+  float bias[8];
+  bias8(o, n, a.N, bias);
+  out_rows<TL>(gemm_lds, acc, [](auto) {}, [&](int r, const float* p) {
+    if (mw + r >= a.M || n >= a.N) return;
+    float z[8];
+    lds8(p, z);
+    out8(o, mw + r, n, a.N, z, bias, alpha);
+  });
 }
 
 template <typename TL, bool MT, bool NT>

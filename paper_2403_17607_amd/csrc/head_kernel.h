@@ -180,7 +180,7 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_prob_kernel(const HeadArgs a
   gemm_loop<TL, false, true>(a.h, a.w, m0, n0, 0, a.D, head_lds, acc);
   uint16_t* P = a.P + mw * a.ldp + nw + 8 * (lane % (COLS / 8));  // ldp: a multiple of 8, at least V
   const bool in = nw + 8 * (lane % (COLS / 8)) < a.V;
-  out_rows<TL, 8>(head_lds, acc, [&](auto mc) {
+  out_rows<TL>(head_lds, acc, [&](auto mc) {
     constexpr int m = decltype(mc)::value;
     const int64_t row = row0 + 16 * m;
     const float lse = row < a.M ? a.lse2[row] : __builtin_inff();
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_prob_kernel(const HeadArgs a
 }
 
 // P of the first piece from what head_lse_kernel kept of it, in place.  Wave
-// w of block (x, y): row 4 x + w, columns 4096 y .. + 4095, 512 at a time; G:
+// w of block (x, y): row 4 x + w, columns 1024 y .. + 1023, 512 at a time; G:
 // columns per reference.
 template <bool DISTILL, int G>
 __global__ __launch_bounds__(256) void head_scale_kernel(const HeadArgs a) {
@@ -213,9 +213,9 @@ __global__ __launch_bounds__(256) void head_scale_kernel(const HeadArgs a) {
   const int lane = threadIdx.x & 63;
   const float lse = a.lse2[row];
   const bool live = lse != __builtin_inff();
-  const int c1 = (int)(blockIdx.y + 1) * 4096 < a.keep ? (int)(blockIdx.y + 1) * 4096 : a.keep;
+  const int c1 = (int)(blockIdx.y + 1) * 1024 < a.keep ? (int)(blockIdx.y + 1) * 1024 : a.keep;
 #pragma unroll 2
-  for (int c0 = blockIdx.y * 4096; c0 < c1; c0 += 512) {
+  for (int c0 = blockIdx.y * 1024; c0 < c1; c0 += 512) {
     const int c = c0 + 8 * lane;
     if (c >= c1) continue;
     uint16_t* p = a.P + row * a.ldp + c;
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(256) void head_scale_kernel(const HeadArgs a) {
 template <typename TL, bool DISTILL>
 hipError_t launch_head_tile(HeadPass pass, const HeadArgs& a, hipStream_t s) {
   if (pass == HEAD_SCALE) {
-    hipLaunchKernelGGL((head_scale_kernel<DISTILL, TL::NB * 16>), dim3((unsigned)((a.M + 3) / 4), (unsigned)((a.keep + 4095) / 4096)),
+    hipLaunchKernelGGL((head_scale_kernel<DISTILL, TL::NB * 16>), dim3((unsigned)((a.M + 3) / 4), (unsigned)((a.keep + 1023) / 1024)),
                        dim3(256), 0, s, a);
     return hipGetLastError();
   }

@@ -21,19 +21,6 @@ size_t type_size(int t) { return t == MLP_FP32 ? 4 : 2; }
 // Row stride of a matrix of `cols` columns.
 bool valid_ld(int64_t ld, int64_t cols) { return ld >= cols && ld <= kMaxDim; }
 
-// Whether rows ld elements apart allow accesses of four columns (16-byte ones
-// of eight).
-bool four_wide(const void* p, int64_t ld, int type) { return !p || (ld % 4 == 0 && aligned(p, 4 * type_size(type))); }
-bool eight_wide(const void* p, int64_t ld, int type) { return !p || (ld * type_size(type) % 16 == 0 && aligned(p, 16)); }
-
-// Fills in which accesses a product's output allows.
-void set_vec(GemmOut& o, int64_t N) {
-  const int t = o.c_fp32 ? MLP_FP32 : MLP_BF16;
-  o.vec = four_wide(o.C, o.ldc, t) && four_wide(o.R, o.ldr, t) && four_wide(o.stash, N, MLP_FP32) && four_wide(o.add, o.ldadd, MLP_FP32);
-  o.vec8 = N % 8 == 0 && eight_wide(o.C, o.ldc, t) && eight_wide(o.R, o.ldr, t) && eight_wide(o.stash, N, MLP_FP32) &&
-           eight_wide(o.add, o.ldadd, MLP_FP32);
-}
-
 SideArgs side(const void* p, int64_t ld, int64_t rows, int64_t cols) {
   return SideArgs{static_cast<const uint16_t*>(p), ld, rows, cols};
 }
@@ -201,7 +188,6 @@ int run_head(bool distill, HeadArgs a, RowLossArgs r, const HeadWs& w, uint8_t* 
         g.out.ldc = lddh;
         g.out.c_fp32 = dh_type == MLP_FP32;
       }
-      set_vec(g.out, D);
       e = launch_gemm(GEMM_DX, g, partial, s);
       if (e != hipSuccess) return hip_fail(e, "dH product launch");
     }
@@ -215,11 +201,20 @@ int run_head(bool distill, HeadArgs a, RowLossArgs r, const HeadWs& w, uint8_t* 
     g.out.C = static_cast<uint8_t*>(dW) + (size_t)v0 * type_size(dw_type);
     g.out.ldc = lddw;
     g.out.c_fp32 = dw_type == MLP_FP32;
-    set_vec(g.out, n);
     e = launch_gemm(GEMM_DW, g, partial, s);
     if (e != hipSuccess) return hip_fail(e, "dW product launch");
   }
   return MLP_OK;
+}
+
+// What an entry point returns for a C++ exception (host memory ran out): none
+// leaves the library.
+int entry_failed() noexcept {
+  try {
+    return fail(MLP_ERR_HIP, "out of host memory");
+  } catch (...) {
+    return MLP_ERR_HIP;
+  }
 }
 
 }  // namespace
@@ -234,7 +229,7 @@ size_t mlp_layer_norm_workspace_bytes(int64_t M, int64_t N, int mode) {
 }
 
 int mlp_layer_norm_forward(const void* X, int x_type, int64_t ldx, const float* gamma, const float* beta, void* Y, int y_type,
-                           int64_t ldy, float* stats, int64_t M, int64_t N, float eps, void* stream) {
+                           int64_t ldy, float* stats, int64_t M, int64_t N, float eps, void* stream) try {
   clear_error();
   if (M < 0 || M > kMaxRows) return fail(MLP_ERR_INVALID_ARG, "M = %lld outside [0, 2^30]", (long long)M);
   if (N < 1 || N > kMaxDim) return fail(MLP_ERR_INVALID_ARG, "N = %lld outside [1, %d]", (long long)N, (int)MLP_MAX_DIM);
@@ -260,11 +255,13 @@ int mlp_layer_norm_forward(const void* X, int x_type, int64_t ldx, const float* 
   a.N = (int)N;
   const hipError_t e = launch_norm_forward(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? MLP_OK : hip_fail(e, "layer norm kernel launch");
+} catch (...) {
+  return entry_failed();
 }
 
 int mlp_layer_norm_backward(const void* X, int x_type, int64_t ldx, const float* gamma, const float* stats, const void* dY, int dy_type,
                             int64_t lddy, void* dX, int dx_type, int64_t lddx, float* dgamma, float* dbeta, int64_t M, int64_t N,
-                            void* ws, void* stream) {
+                            void* ws, void* stream) try {
   clear_error();
   if (M < 0 || M > kMaxRows) return fail(MLP_ERR_INVALID_ARG, "M = %lld outside [0, 2^30]", (long long)M);
   if (N < 1 || N > kMaxDim) return fail(MLP_ERR_INVALID_ARG, "N = %lld outside [1, %d]", (long long)N, (int)MLP_MAX_DIM);
@@ -302,6 +299,8 @@ int mlp_layer_norm_backward(const void* X, int x_type, int64_t ldx, const float*
     e = launch_norm_backward(a, s);
   }
   return e == hipSuccess ? MLP_OK : hip_fail(e, "layer norm backward launch");
+} catch (...) {
+  return entry_failed();
 }
 
 // ------------------------------------------------------------------ dense --
@@ -314,7 +313,7 @@ size_t mlp_dense_workspace_bytes(int64_t M, int64_t K, int64_t N, int mode) {
 
 int mlp_dense_forward(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_t ldw, const float* bias, int activation, const void* R,
                       int64_t ldr, void* Y, int y_type, int64_t ldy, float* stash, int64_t M, int64_t K, int64_t N, void* ws,
-                      void* stream) {
+                      void* stream) try {
   clear_error();
   if (M < 0 || M > kMaxRows) return fail(MLP_ERR_INVALID_ARG, "M = %lld outside [0, 2^30]", (long long)M);
   if (K < 1 || K > kMaxDim || N < 1 || N > kMaxDim)
@@ -344,14 +343,15 @@ int mlp_dense_forward(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_t
   g.out.C = Y;
   g.out.ldc = ldy;
   g.out.c_fp32 = y_type == MLP_FP32;
-  set_vec(g.out, N);
   const hipError_t e = launch_gemm(GEMM_XW, g, static_cast<float*>(ws), static_cast<hipStream_t>(stream));
   return e == hipSuccess ? MLP_OK : hip_fail(e, "dense product launch");
+} catch (...) {
+  return entry_failed();
 }
 
 int mlp_dense_backward(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_t ldw, int activation, const float* stash,
                        const void* dY, int dy_type, int64_t lddy, void* dX, int dx_type, int64_t lddx, void* dW, int dw_type,
-                       int64_t lddw, float* db, int64_t M, int64_t K, int64_t N, void* ws_, void* stream) {
+                       int64_t lddw, float* db, int64_t M, int64_t K, int64_t N, void* ws_, void* stream) try {
   clear_error();
   if (M < 0 || M > kMaxRows) return fail(MLP_ERR_INVALID_ARG, "M = %lld outside [0, 2^30]", (long long)M);
   if (K < 1 || K > kMaxDim || N < 1 || N > kMaxDim)
@@ -403,7 +403,6 @@ int mlp_dense_backward(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_
     g.out.C = dX;
     g.out.ldc = lddx;
     g.out.c_fp32 = dx_type == MLP_FP32;
-    set_vec(g.out, K);
     e = launch_gemm(GEMM_DX, g, partial, s);
     if (e != hipSuccess) return hip_fail(e, "dX product launch");
   }
@@ -418,11 +417,12 @@ int mlp_dense_backward(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_
     g.out.C = dW;
     g.out.ldc = lddw;
     g.out.c_fp32 = dw_type == MLP_FP32;
-    set_vec(g.out, N);
     e = launch_gemm(GEMM_DW, g, partial, s);
     if (e != hipSuccess) return hip_fail(e, "dW product launch");
   }
   return MLP_OK;
+} catch (...) {
+  return entry_failed();
 }
 
 // ------------------------------------------------------------------- head --
@@ -435,7 +435,7 @@ size_t mlp_head_workspace_bytes(int64_t M, int64_t D, int64_t V, int top, int mo
 
 int mlp_cross_entropy(const uint16_t* H, int64_t ldh, const uint16_t* W, int64_t ldw, const int64_t* target, int64_t ignore_index,
                       float* loss, float* row_loss, void* dH, int dh_type, int64_t lddh, void* dW, int dw_type, int64_t lddw,
-                      int64_t M, int64_t D, int64_t V, void* ws, void* stream) {
+                      int64_t M, int64_t D, int64_t V, void* ws, void* stream) try {
   clear_error();
   if (int rc = check_head(H, ldh, W, ldw, dH, dh_type, lddh, dW, dw_type, lddw, loss, row_loss, M, D, V, ws)) return rc;
   if (M > 0 && !target) return fail(MLP_ERR_INVALID_ARG, "null target");
@@ -459,11 +459,13 @@ int mlp_cross_entropy(const uint16_t* H, int64_t ldh, const uint16_t* W, int64_t
   r.loss = loss;
   r.row_loss = row_loss;
   return run_head(false, a, r, w, static_cast<uint8_t*>(ws), dH, dh_type, lddh, dW, dw_type, lddw, static_cast<hipStream_t>(stream));
+} catch (...) {
+  return entry_failed();
 }
 
 int mlp_distill(const uint16_t* H, int64_t ldh, const uint16_t* W, int64_t ldw, const int64_t* index, const void* logits,
                 int logits_type, int top, float temperature, float* loss, float* row_loss, void* dH, int dh_type, int64_t lddh,
-                void* dW, int dw_type, int64_t lddw, int64_t M, int64_t D, int64_t V, void* ws_, void* stream) {
+                void* dW, int dw_type, int64_t lddw, int64_t M, int64_t D, int64_t V, void* ws_, void* stream) try {
   clear_error();
   if (int rc = check_head(H, ldh, W, ldw, dH, dh_type, lddh, dW, dw_type, lddw, loss, row_loss, M, D, V, ws_)) return rc;
   if (top < 1 || top > kHeadMaxTop) return fail(MLP_ERR_INVALID_ARG, "top = %d outside [1, %d]", top, kHeadMaxTop);
@@ -512,6 +514,8 @@ int mlp_distill(const uint16_t* H, int64_t ldh, const uint16_t* W, int64_t ldw, 
   r.loss = loss;
   r.row_loss = row_loss;
   return run_head(true, a, r, w, ws, dH, dh_type, lddh, dW, dw_type, lddw, s);
+} catch (...) {
+  return entry_failed();
 }
 
 }  // extern "C"

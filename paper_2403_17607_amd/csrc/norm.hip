@@ -175,15 +175,6 @@ __device__ __forceinline__ int64_t uniform(int64_t v) {
 __device__ __forceinline__ void fill_columns(float* dst, int cols, const float* src, int N, float missing) {
   for (int c = threadIdx.x; c < cols; c += blockDim.x) dst[c] = c < N ? (src ? src[c] : missing) : 0.f;
 }
-__device__ __forceinline__ void lds8(const float* p, float (&v)[8]) {
-  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    v[q] = a[q];
-    v[q + 4] = b[q];
-  }
-}
-
 }  // namespace
 
 // Threads of a forward workgroup.

@@ -38,6 +38,15 @@ __device__ __forceinline__ void load8(const float* p, int n, float (&v)[8]) {
     for (int q = 0; q < 8; ++q) v[q] = q < n ? p[q] : 0.f;
   }
 }
+// eight floats in LDS, 16-byte aligned
+__device__ __forceinline__ void lds8(const float* p, float (&v)[8]) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    v[q] = a[q];
+    v[q + 4] = b[q];
+  }
+}
 __device__ __forceinline__ void store8(uint16_t* p, int n, const float (&v)[8]) {
   const u32x4 x = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
   if (n >= 8) {

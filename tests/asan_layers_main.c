@@ -67,7 +67,7 @@ static int refusals(void) {
   CHECK(DF(p, 7, p, 8, 0, NULL, 0, p, b, NULL, 4, 8, 8, p) == inv && DF(p, 8, p, 7, 0, NULL, 0, p, b, NULL, 4, 8, 8, p) == inv);
   CHECK(DF(p, 8, p, 8, 0, p, 7, p, b, NULL, 4, 8, 8, p) == inv && DF(p, 8, p, 8, 0, q, 8, p, b, NULL, 4, 8, 8, p) == inv);
   CHECK(DF(NULL, 8, p, 8, 0, NULL, 0, p, b, NULL, 4, 8, 8, p) == inv && DF(p, 8, p, 8, 4, NULL, 0, p, b, q, 4, 8, 8, p) == inv);
-  CHECK(DF(p, 4096, p, 64, 0, NULL, 0, p, b, NULL, 1, 4096, 64, NULL) == MLP_ERR_WORKSPACE);
+  CHECK(DF(p, 4096, p, 64, 0, NULL, 0, p, b, NULL, 2, 4096, 64, NULL) == MLP_ERR_WORKSPACE); /* one row needs none */
   CHECK(DF(NULL, 0, NULL, 0, 0, NULL, 0, NULL, b, NULL, 0, 8, 8, NULL) == MLP_OK);
 #define DB(X, W, act, st, dY, dyt, dX, dW, lddw, M, ws) mlp_dense_backward(X, 8, W, 8, act, st, dY, dyt, 8, dX, b, 8, dW, b, lddw, p, M, 8, 8, ws, NULL)
   CHECK(DB(p, p, 1, NULL, p, b, p, p, 8, 4, p) == inv && DB(p, p, 0, NULL, NULL, b, p, p, 8, 4, p) == inv);

@@ -250,7 +250,7 @@ def dense_case(ffmlp, M, K, N, act="linear", yt=BF, gt=F32, dyt=BF, bias=True, r
     close_norm(dW, ref, (math.sqrt(M + 8) * U) * s.norm() + (dzb + HALF[gt]) * ref.norm() + 1e-12, "dW norm")
 
 
-SIZES = [(1, 1, 1), (1, 16, 8), (2, 3, 5), (7, 31, 33), (16, 64, 64), (17, 65, 130), (64, 128, 128), (65, 200, 136),
+SIZES = [(1, 1, 1), (1, 16, 8), (1, 777, 8200), (1, 100, 16401), (2, 3, 5), (7, 31, 33), (16, 64, 64), (17, 65, 130), (64, 128, 128), (65, 200, 136),
          (130, 96, 257), (16, 1000, 1003), (1, 2048, 512), (5, 4097, 129), (300, 520, 264), (129, 1032, 1000)]
 
 
@@ -314,6 +314,23 @@ def test_dense_relu_masks_what_is_not_finite(ffmlp, gpu):
     dY[0, 3], dY[1, 3] = float("inf"), float("nan")
     dX, dW, db = layer.backward(W, X, dY, ws, stash=stash)
     assert torch.isfinite(dX).all() and torch.isfinite(dW).all() and db[3] == 0
+
+
+def test_more_than_2_31_elements(ffmlp, gpu):
+    """Offsets past 32 bits: the last rows of a 66000 x 33000 output, and of a
+    norm of as many elements."""
+    g = gen(17)
+    M, K, N = 66000, 16, 33000
+    X, W = randn(g, M, K), randn(g, K, N)
+    layer = ffmlp.Dense(K, N, "relu")
+    Y = layer.forward(W, X, ws=layer.workspace(M, mode=ffmlp.MLP_MODE_INFER))
+    rows = torch.tensor([0, 1, M // 2, M - 2, M - 1], device="cuda")
+    ref = (X[rows].double() @ W.double()).clamp_min(0)
+    close(Y[rows], ref, (K + 8) * U * (X[rows].double().abs() @ W.double().abs()) + HALF[BF] * ref + 1e-12, "Y")
+    Z = ffmlp.LayerNorm(N).forward(Y)
+    y = Y[rows].double()
+    ref = (y - y.mean(1, keepdim=True)) / (y.var(1, unbiased=False, keepdim=True) + 1e-5).sqrt()
+    close(Z[rows], ref, (HALF[BF] + 200 * U) * ref.abs() + 200 * U, "Z")
 
 
 # ---------------------------------------------------------- vocabulary losses --
@@ -393,6 +410,17 @@ def test_cross_entropy(ffmlp, gpu, M, D, V):
 @pytest.mark.parametrize("M,D,V", [(2048, 128, 5000), (2050, 64, 4101), (1025, 200, 8192)])
 def test_cross_entropy_large_tiles(ffmlp, gpu, M, D, V):
     ce_case(ffmlp, M, D, V)
+
+
+def test_cross_entropy_in_pieces(ffmlp, gpu):
+    """More logits than a piece holds (2^29): the second piece's are computed
+    again, dH adds up over both."""
+    assert 9000 * 66001 > 1 << 29
+    ce_case(ffmlp, 9000, 16, 66001)
+
+
+def test_distill_in_pieces(ffmlp, gpu):
+    distill_case(ffmlp, 8200, 8, 65544, 3, 2.0, gt=BF)
 
 
 @pytest.mark.parametrize("offset,extra", [(1, 0), (8, 8), (3, 5)])
