@@ -27,6 +27,7 @@ struct GemmOut {
   void* C;             // [M][ldc], bf16 or fp32
   int64_t ldc;
   int c_fp32;
+  int nt;              // non-temporal stores of C
 };
 
 struct GemmArgs {

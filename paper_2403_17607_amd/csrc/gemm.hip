@@ -217,20 +217,24 @@ __global__ __launch_bounds__(256) void delta_kernel(const DeltaArgs a) {
   float db[8] = {};
   if (c < a.N) {
     const int n = a.N - c < 8 ? a.N - c : 8;
-#pragma unroll 2
-    for (int64_t r = r0 + wave; r < r1; r += 4) {
-      float v[8];
-      if constexpr (F32) load8(static_cast<const float*>(a.dY) + r * a.lddy + c, n, v);
-      else load8(static_cast<const uint16_t*>(a.dY) + r * a.lddy + c, n, v);
-      if (a.stash) {
-        float d[8];
-        load8(a.stash + r * a.N + c, n, d);
+    for (int64_t r = r0 + wave; r < r1; r += 16) {  // four rows in flight
+      float v[4][8], d[4][8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = a.relu && d[q] == 0.f ? 0.f : v[q] * d[q];
+      for (int k = 0; k < 4; ++k) {
+        const int nk = r + 4 * k < r1 ? n : 0;
+        if constexpr (F32) load8(static_cast<const float*>(a.dY) + (r + 4 * k) * a.lddy + c, nk, v[k]);
+        else load8(static_cast<const uint16_t*>(a.dY) + (r + 4 * k) * a.lddy + c, nk, v[k]);
+        if (a.stash) load8(a.stash + (r + 4 * k) * a.N + c, nk, d[k]);
       }
 #pragma unroll
-      for (int q = 0; q < 8; ++q) db[q] += v[q];
-      if (a.dZ) store8(a.dZ + r * a.ldz + c, n, v);
+      for (int k = 0; k < 4; ++k) {
+        if (a.stash)
+#pragma unroll
+          for (int q = 0; q < 8; ++q) v[k][q] = a.relu && d[k][q] == 0.f ? 0.f : v[k][q] * d[k][q];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) db[q] += v[k][q];
+        if (a.dZ && r + 4 * k < r1) store8(a.dZ + (r + 4 * k) * a.ldz + c, n, v[k]);
+      }
     }
   }
   if (!a.db) return;

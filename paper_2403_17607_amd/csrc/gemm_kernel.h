@@ -390,7 +390,7 @@ __device__ __forceinline__ void out8(const GemmOut& o, int64_t m, int n, int N, 
       act8<false>(o.act, z, d);
     } else {
       act8<true>(o.act, z, d);
-      store8(o.stash + m * (int64_t)N + n, left, d);
+      store8<true>(o.stash + m * (int64_t)N + n, left, d);
     }
   }
   if (o.R) {
@@ -399,8 +399,13 @@ __device__ __forceinline__ void out8(const GemmOut& o, int64_t m, int n, int N, 
 #pragma unroll
     for (int q = 0; q < 8; ++q) z[q] += v[q];
   }
-  if (o.c_fp32) store8(static_cast<float*>(o.C) + m * o.ldc + n, left, z);
-  else store8(static_cast<uint16_t*>(o.C) + m * o.ldc + n, left, z);
+  if (o.nt) {
+    if (o.c_fp32) store8<true>(static_cast<float*>(o.C) + m * o.ldc + n, left, z);
+    else store8<true>(static_cast<uint16_t*>(o.C) + m * o.ldc + n, left, z);
+  } else {
+    if (o.c_fp32) store8(static_cast<float*>(o.C) + m * o.ldc + n, left, z);
+    else store8(static_cast<uint16_t*>(o.C) + m * o.ldc + n, left, z);
+  }
 }
 
 // C = the product, or one split's share of it as fp32 partial sums.

@@ -30,22 +30,10 @@ struct HeadArgs {
   int64_t ldp;
   int keep;               // columns of the first piece, or 0: no gradients
   float* ref;             // [keep / the columns of a wave's tile][M]
+  int chunk;              // columns of a row that a wave of HEAD_SCALE takes
 };
 
-// The passes over the logits: log-sum-exp; P of the first piece from what that
-// kept; P of a later piece.
-enum HeadPass { HEAD_LSE, HEAD_SCALE, HEAD_PROB };
 
-struct HeadPlan {
-  bool large;
-  int mt, nt, runs, per_run;  // head_lse_kernel
-  int piece, pieces;          // columns of P, a multiple of 256 unless one piece holds all
-  int refs;                   // references of a row in the first piece
-};
-HeadPlan head_plan(int64_t M, int64_t D, int64_t V);
-
-hipError_t launch_head_ce(HeadPass pass, bool large, const HeadArgs& a, hipStream_t s);
-hipError_t launch_head_distill(HeadPass pass, bool large, const HeadArgs& a, hipStream_t s);
 
 // The teacher's entries: probabilities over a row's list, sorted by index,
 // and the table of starts.  ok[m]: 1, 0 (an empty list) or -1 (an index past
@@ -65,6 +53,7 @@ struct TeacherArgs {
 hipError_t launch_teacher(const TeacherArgs& a, hipStream_t s);
 
 // lse2 and the loss of every row, then the mean loss and the gradient's scale.
+// Rows: launch_row_loss, or HEAD_SCALE on its way.
 struct RowLossArgs {
   const f32x2* partial;
   int parts;
@@ -81,6 +70,21 @@ struct RowLossArgs {
   float *loss, *alpha;    // mean loss; T / rows that count
 };
 hipError_t launch_row_loss(const RowLossArgs& a, hipStream_t s);
+hipError_t launch_mean_loss(const RowLossArgs& a, hipStream_t s);
+
+struct HeadPlan {
+  bool large;
+  int mt, nt, runs, per_run;  // head_lse_kernel
+  int piece, pieces;          // columns of P, a multiple of 256 unless one piece holds all
+  int refs;                   // references of a row in the first piece
+};
+HeadPlan head_plan(int64_t M, int64_t D, int64_t V);
+
+// The passes over the logits: log-sum-exp; P of the first piece from what that
+// kept, and the losses of the rows (r); P of a later piece.
+enum HeadPass { HEAD_LSE, HEAD_SCALE, HEAD_PROB };
+hipError_t launch_head_ce(HeadPass pass, bool large, const HeadArgs& a, const RowLossArgs& r, hipStream_t s);
+hipError_t launch_head_distill(HeadPass pass, bool large, const HeadArgs& a, const RowLossArgs& r, hipStream_t s);
 
 #ifdef __HIPCC__
 // (m, s) and (m2, s2), each a maximum and a sum of 2^(x - maximum), as one.
@@ -88,6 +92,48 @@ __device__ __forceinline__ void head_merge(float& m, float& s, float m2, float s
   const float top = __builtin_fmaxf(m, m2), at = top == -__builtin_inff() ? 0.f : top;
   s = s * __builtin_amdgcn_exp2f(m - at) + s2 * __builtin_amdgcn_exp2f(m2 - at);
   m = top;
+}
+
+// A row's partial sums merged in a fixed tree by a wave, and its loss.  Returns
+// its lse in base 2 (+inf: the row does not count); `write`: also to memory.
+__device__ __forceinline__ float row_loss(const RowLossArgs& a, int64_t row, int lane, bool write) {
+  constexpr float kLn2 = 0.69314718f;
+  float m = -__builtin_inff(), s = 0.f;
+  for (int p = lane; p < a.parts; p += 64) {
+    const f32x2 v = a.partial[(int64_t)p * a.M + row];
+    head_merge(m, s, v[0], v[1]);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) head_merge(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
+  float lse = m + __builtin_amdgcn_logf(s), loss = 0.f;  // logf: base 2
+  int state;  // 1 counts, 0 does not, -1 has an index past the vocabulary
+  if (a.q) {
+    state = a.ok[row];
+    if (write) {
+      for (int e = lane; e < a.top; e += 64) {
+        const float q = a.q[row * a.top + e];
+        if (!(q == 0.f)) loss += q * (kLn2 * (lse - a.pick[row * a.top + e] + __builtin_amdgcn_logf(q)));
+      }
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) loss += __shfl_xor(loss, d);
+      loss *= a.t2;
+    }
+  } else {
+    const int64_t t = a.target[row];
+    state = t == a.ignore ? 0 : t >= 0 && t < a.V ? 1 : -1;
+    if (state == 1) loss = kLn2 * (lse - a.pick[row]);
+  }
+  if (state == 0) {
+    lse = __builtin_inff();
+    loss = 0.f;
+  } else if (state < 0) {
+    lse = loss = __builtin_nanf("");
+  }
+  if (write && lane == 0) {
+    a.lse2[row] = lse;
+    a.row_loss[row] = loss;
+  }
+  return lse;
 }
 #endif
 

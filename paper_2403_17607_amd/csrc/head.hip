@@ -90,44 +90,10 @@ hipError_t launch_teacher(const TeacherArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// One wave per row: its partial sums merged in a fixed tree, then its loss.
+// One wave per row.
 __global__ __launch_bounds__(256) void row_loss_kernel(const RowLossArgs a) {
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (row >= a.M) return;
-  float m = -__builtin_inff(), s = 0.f;
-  for (int p = lane; p < a.parts; p += 64) {
-    const f32x2 v = a.partial[(int64_t)p * a.M + row];
-    head_merge(m, s, v[0], v[1]);
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) head_merge(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
-  float lse = m + __builtin_amdgcn_logf(s), loss = 0.f;  // logf: base 2
-  int state;  // 1 counts, 0 does not, -1 has an index past the vocabulary
-  if (a.q) {
-    state = a.ok[row];
-    for (int e = lane; e < a.top; e += 64) {
-      const float q = a.q[row * a.top + e];
-      if (!(q == 0.f)) loss += q * (kLn2 * (lse - a.pick[row * a.top + e] + __builtin_amdgcn_logf(q)));
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) loss += __shfl_xor(loss, d);
-    loss *= a.t2;
-  } else {
-    const int64_t t = a.target[row];
-    state = t == a.ignore ? 0 : t >= 0 && t < a.V ? 1 : -1;
-    if (state == 1) loss = kLn2 * (lse - a.pick[row]);
-  }
-  if (state == 0) {
-    lse = __builtin_inff();
-    loss = 0.f;
-  } else if (state < 0) {
-    lse = loss = __builtin_nanf("");
-  }
-  if (lane == 0) {
-    a.lse2[row] = lse;
-    a.row_loss[row] = loss;
-  }
+  if (row < a.M) row_loss(a, row, threadIdx.x & 63, true);
 }
 
 // One workgroup: thread t adds rows t, t + 1024, ... in order, then a tree.
@@ -159,11 +125,12 @@ __global__ __launch_bounds__(1024) void mean_loss_kernel(const RowLossArgs a) {
 }
 
 hipError_t launch_row_loss(const RowLossArgs& a, hipStream_t s) {
-  if (a.M > 0) {
-    hipLaunchKernelGGL(row_loss_kernel, dim3((unsigned)cdiv(a.M, 4)), dim3(256), 0, s, a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
+  if (a.M == 0) return hipSuccess;
+  hipLaunchKernelGGL(row_loss_kernel, dim3((unsigned)cdiv(a.M, 4)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_mean_loss(const RowLossArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(mean_loss_kernel, dim3(1), dim3(1024), 0, s, a);
   return hipGetLastError();
 }

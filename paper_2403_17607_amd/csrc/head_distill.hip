@@ -3,8 +3,8 @@
 
 namespace ffmlp {
 
-hipError_t launch_head_distill(HeadPass pass, bool large, const HeadArgs& a, hipStream_t s) {
-  return launch_head<true>(pass, large, a, s);
+hipError_t launch_head_distill(HeadPass pass, bool large, const HeadArgs& a, const RowLossArgs& r, hipStream_t s) {
+  return launch_head<true>(pass, large, a, r, s);
 }
 
 }  // namespace ffmlp

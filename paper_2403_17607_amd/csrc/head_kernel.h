@@ -22,8 +22,6 @@
 
 namespace ffmlp {
 
-constexpr float kLn2 = 0.69314718f;
-
 // f(column within the wave's columns, position in the row's list) for row
 // `row`'s entries among `cols` columns from c0 on, c0 a multiple of 64.
 template <bool DISTILL, typename F>
@@ -204,18 +202,19 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_prob_kernel(const HeadArgs a
 }
 
 // P of the first piece from what head_lse_kernel kept of it, in place.  Wave
-// w of block (x, y): row 4 x + w, columns 1024 y .. + 1023, 512 at a time; G:
-// columns per reference.
+// w of block (x, y): row 4 x + w, columns `chunk` y on, 512 at a time; G: columns
+// per reference.  Each wave merges its row's sums itself and those of y = 0 write
+// the row's loss: one launch less.
 template <bool DISTILL, int G>
-__global__ __launch_bounds__(256) void head_scale_kernel(const HeadArgs a) {
+__global__ __launch_bounds__(256) void head_scale_kernel(const HeadArgs a, const RowLossArgs rl) {
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= a.M) return;
   const int lane = threadIdx.x & 63;
-  const float lse = a.lse2[row];
+  const float lse = row_loss(rl, row, lane, blockIdx.y == 0);
   const bool live = lse != __builtin_inff();
-  const int c1 = (int)(blockIdx.y + 1) * 1024 < a.keep ? (int)(blockIdx.y + 1) * 1024 : a.keep;
+  const int c1 = (int)(blockIdx.y + 1) * a.chunk < a.keep ? (int)(blockIdx.y + 1) * a.chunk : a.keep;
 #pragma unroll 2
-  for (int c0 = blockIdx.y * 1024; c0 < c1; c0 += 512) {
+  for (int c0 = blockIdx.y * a.chunk; c0 < c1; c0 += 512) {
     const int c = c0 + 8 * lane;
     if (c >= c1) continue;
     uint16_t* p = a.P + row * a.ldp + c;
@@ -238,10 +237,10 @@ __global__ __launch_bounds__(256) void head_scale_kernel(const HeadArgs a) {
 }
 
 template <typename TL, bool DISTILL>
-hipError_t launch_head_tile(HeadPass pass, const HeadArgs& a, hipStream_t s) {
+hipError_t launch_head_tile(HeadPass pass, const HeadArgs& a, const RowLossArgs& r, hipStream_t s) {
   if (pass == HEAD_SCALE) {
-    hipLaunchKernelGGL((head_scale_kernel<DISTILL, TL::NB * 16>), dim3((unsigned)((a.M + 3) / 4), (unsigned)((a.keep + 1023) / 1024)),
-                       dim3(256), 0, s, a);
+    hipLaunchKernelGGL((head_scale_kernel<DISTILL, TL::NB * 16>), dim3((unsigned)((a.M + 3) / 4), (unsigned)((a.keep + a.chunk - 1) / a.chunk)),
+                       dim3(256), 0, s, a, r);
     return hipGetLastError();
   }
   constexpr int lds = gemm_lds_bytes<TL, false, true>();
@@ -254,8 +253,8 @@ hipError_t launch_head_tile(HeadPass pass, const HeadArgs& a, hipStream_t s) {
 }
 
 template <bool DISTILL>
-hipError_t launch_head(HeadPass pass, bool large, const HeadArgs& a, hipStream_t s) {
-  return large ? launch_head_tile<GemmLarge, DISTILL>(pass, a, s) : launch_head_tile<GemmMedium, DISTILL>(pass, a, s);
+hipError_t launch_head(HeadPass pass, bool large, const HeadArgs& a, const RowLossArgs& r, hipStream_t s) {
+  return large ? launch_head_tile<GemmLarge, DISTILL>(pass, a, r, s) : launch_head_tile<GemmMedium, DISTILL>(pass, a, r, s);
 }
 
 }  // namespace ffmlp

@@ -136,11 +136,7 @@ int run_head(bool distill, HeadArgs a, RowLossArgs r, const HeadWs& w, uint8_t* 
     a.ldp = w.ldp;
     a.keep = w.plan.piece;
     a.ref = reinterpret_cast<float*>(ws + w.ref);
-  }
-  hipError_t e;
-  if (M > 0) {
-    e = launch(HEAD_LSE, w.plan.large, a, s);
-    if (e != hipSuccess) return hip_fail(e, "log-sum-exp kernel launch");
+    a.chunk = M >= 4096 ? 4096 : 1024;  // few rows: more waves (513 rows, 10007 words: 11 -> 8 us)
   }
   r.partial = a.partial;
   r.parts = w.plan.runs * 2;
@@ -150,8 +146,15 @@ int run_head(bool distill, HeadArgs a, RowLossArgs r, const HeadWs& w, uint8_t* 
   r.lse2 = reinterpret_cast<float*>(ws + w.lse2);
   if (!r.row_loss) r.row_loss = reinterpret_cast<float*>(ws + w.row_loss);
   r.alpha = reinterpret_cast<float*>(ws + w.alpha);
-  e = launch_row_loss(r, s);
-  if (e != hipSuccess) return hip_fail(e, "row loss kernel launch");
+  hipError_t e;
+  if (M > 0) {
+    e = launch(HEAD_LSE, w.plan.large, a, r, s);
+    if (e != hipSuccess) return hip_fail(e, "log-sum-exp kernel launch");
+    e = dW ? launch(HEAD_SCALE, w.plan.large, a, r, s) : launch_row_loss(r, s);
+    if (e != hipSuccess) return hip_fail(e, "row loss kernel launch");
+  }
+  e = launch_mean_loss(r, s);
+  if (e != hipSuccess) return hip_fail(e, "mean loss kernel launch");
   if (!dW) return MLP_OK;
   float* partial = reinterpret_cast<float*>(ws + w.partial);
   float* acc = reinterpret_cast<float*>(ws + w.acc);
@@ -164,9 +167,9 @@ int run_head(bool distill, HeadArgs a, RowLossArgs r, const HeadWs& w, uint8_t* 
         a.V = n;
         a.col0 = v0;
         a.nt = (int)((n + (w.plan.large ? 255 : 127)) / (w.plan.large ? 256 : 128));
+        e = launch(HEAD_PROB, w.plan.large, a, r, s);
+        if (e != hipSuccess) return hip_fail(e, "logit gradient kernel launch");
       }
-      e = launch(k == 0 ? HEAD_SCALE : HEAD_PROB, w.plan.large, a, s);
-      if (e != hipSuccess) return hip_fail(e, "logit gradient kernel launch");
       // dH: pieces before the last add up in fp32
       GemmArgs g{};
       g.m = side(P, w.ldp, M, n);
@@ -343,6 +346,9 @@ int mlp_dense_forward(const uint16_t* X, int64_t ldx, const uint16_t* W, int64_t
   g.out.C = Y;
   g.out.ldc = ldy;
   g.out.c_fp32 = y_type == MLP_FP32;
+  // Y is not read again here and would only displace X and W from the caches
+  // (8192 x 2048 x 8192 with GELU: 274 -> 259 us); gradients showed no gain.
+  g.out.nt = 1;
   const hipError_t e = launch_gemm(GEMM_XW, g, static_cast<float*>(ws), static_cast<hipStream_t>(stream));
   return e == hipSuccess ? MLP_OK : hip_fail(e, "dense product launch");
 } catch (...) {

@@ -47,20 +47,28 @@ __device__ __forceinline__ void lds8(const float* p, float (&v)[8]) {
     v[q + 4] = b[q];
   }
 }
+template <bool NT = false>
 __device__ __forceinline__ void store8(uint16_t* p, int n, const float (&v)[8]) {
   const u32x4 x = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
   if (n >= 8) {
-    *reinterpret_cast<u32x4_a2*>(p) = x;
+    if (NT) __builtin_nontemporal_store(x, reinterpret_cast<u32x4_a2*>(p));
+    else *reinterpret_cast<u32x4_a2*>(p) = x;
   } else {
 #pragma unroll
     for (int q = 0; q < 8; ++q)
       if (q < n) p[q] = (uint16_t)(x[q / 2] >> (16 * (q & 1)));
   }
 }
+template <bool NT = false>
 __device__ __forceinline__ void store8(float* p, int n, const float (&v)[8]) {
   if (n >= 8) {
-    *reinterpret_cast<f32x4_a4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<f32x4_a4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    if (NT) {
+      __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4_a4*>(p));
+      __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, reinterpret_cast<f32x4_a4*>(p + 4));
+    } else {
+      *reinterpret_cast<f32x4_a4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<f32x4_a4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    }
   } else {
 #pragma unroll
     for (int q = 0; q < 8; ++q)

@@ -62,7 +62,8 @@ def _matrix(t, name, rows, cols, dtypes=(torch.bfloat16,), device=None) -> int:
 def _vector(t, name, n, device, dtype=torch.float32):
     if t is None:
         return None
-    _base._require(t, name, dtype, shape=(n,), device=device)
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == (n,) and t.device == device and t.is_contiguous()):
+        _base._require(t, name, dtype, shape=(n,), device=device)  # says what is wrong
     return t.data_ptr()
 
 
@@ -87,9 +88,14 @@ def _dim(n, name) -> int:
     return n
 
 
+# the current device's index; torch.cuda.current_device() makes sure of the
+# initialisation first, which a tensor on the GPU has done
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _run(fn, dev, *args) -> None:
     """Call fn(*args, stream) with `dev` as the current device."""
-    if dev.index is None or dev.index == torch.cuda.current_device():
+    if dev.index == _current_device():
         rc = fn(*args, _base._stream(dev))
     else:
         with torch.cuda.device(dev):
