@@ -120,7 +120,9 @@ struct Loader {
   // nor empty: their rest would be of the next row (along k: nonzero), or they
   // end with the matrix, where the range check may drop the last element with
   // the dword it shares.
-  __device__ __forceinline__ bool ragged() const { return T ? (a.cols & 7) != 0 : (kend & 7) != 0; }
+  __device__ __forceinline__ bool ragged() const {
+    return T ? (a.cols & 7) != 0 && r0 + S::CH * 8 > a.cols : (kend & 7) != 0;
+  }
   // That step's slice once more, exactly, through registers.
   __device__ __forceinline__ void fix(uint8_t* lds, int64_t k0, int tid) const {
     const int64_t rend = T ? kend : a.rows, cend = T ? a.cols : kend;
