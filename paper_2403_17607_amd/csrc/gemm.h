@@ -42,7 +42,7 @@ struct GemmArgs {
 };
 
 // Workgroup tiles (gemm_kernel.h) and which sides have k across their rows.
-enum { GEMM_ROWS = 0, GEMM_MEDIUM = 1, GEMM_HALF = 2, GEMM_LARGE = 3, GEMM_SQUARE = 4 };
+enum { GEMM_ROWS = 0, GEMM_SMALL = 1, GEMM_MEDIUM = 2, GEMM_HALF = 3, GEMM_LARGE = 4, GEMM_SQUARE = 5 };
 enum { GEMM_XW = 0, GEMM_DX = 1, GEMM_DW = 2 };
 
 struct GemmPlan {

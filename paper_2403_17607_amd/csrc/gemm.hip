@@ -18,7 +18,9 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 //   8192 x 8192 over 2048 (X W): square 265, large 240, half 285
 //   4096 x 1024 over 8192 (X^T dZ): square 191, half 104, medium 90; half with
 //     two splits and their sum 85
-//   1024 x 1024 over 1024 (X W): large 25, half 16, medium 12
+//   1024 x 1024 over 1024 (X W): large 25, half 16, medium 10.1, small 8.1
+//   1111 x 771 over 1283 (dZ W^T): medium 13.5, small 10.8; 1111 x 1283 over 771
+//     (X W): medium 10.1, small 12.4
 struct TileCost {
   int tile, bm, bn, bk, per_cu;
   double alone, shared, rest;
@@ -32,6 +34,7 @@ constexpr TileCost kTiles[] = {
     tile_cost<GemmLarge>(GEMM_LARGE, 2, 0.62, 0.90, 4.0),
     tile_cost<GemmHalf>(GEMM_HALF, 2, 0.75, 1.05, 5.0),
     tile_cost<GemmMedium>(GEMM_MEDIUM, 2, 0.42, 0.66, 4.0),
+    tile_cost<GemmSmall>(GEMM_SMALL, 2, 0.28, 0.50, 3.5),
     tile_cost<GemmRows>(GEMM_ROWS, 2, 0.30, 0.40, 3.0),
 };
 constexpr int kCUs = 256;

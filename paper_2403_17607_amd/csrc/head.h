@@ -23,7 +23,7 @@ struct HeadArgs {
   const uint16_t* start;  // [M][keys]: entries with index < 128 k
   int top, keys;
   float* pick;            // [M][top] logits (base 2) of the entries
-  f32x2* partial;         // [runs * 2][M] maximum and sum
+  f32x2* partial;         // [parts][M] maximum and sum
   int runs, per_run, mt, nt;
   const float* lse2;      // [M]; +inf: the row does not count
   uint16_t* P;            // [M][ldp]
@@ -32,8 +32,6 @@ struct HeadArgs {
   float* ref;             // [keep / the columns of a wave's tile][M]
   int chunk;              // columns of a row that a wave of HEAD_SCALE takes
 };
-
-
 
 // The teacher's entries: probabilities over a row's list, sorted by index,
 // and the table of starts.  ok[m]: 1, 0 (an empty list) or -1 (an index past
@@ -75,10 +73,11 @@ hipError_t launch_mean_loss(const RowLossArgs& a, hipStream_t s);
 struct HeadPlan {
   bool large;
   int mt, nt, runs, per_run;  // head_lse_kernel
+  int parts;                  // its maxima and sums of a row
   int piece, pieces;          // columns of P, a multiple of 256 unless one piece holds all
   int refs;                   // references of a row in the first piece
 };
-HeadPlan head_plan(int64_t M, int64_t D, int64_t V);
+HeadPlan head_plan(int64_t M, int64_t V);
 
 // The passes over the logits: log-sum-exp; P of the first piece from what that
 // kept, and the losses of the rows (r); P of a later piece.

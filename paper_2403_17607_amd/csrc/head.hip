@@ -8,7 +8,7 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t kPieceElems = (int64_t)1 << 29;  // P of a piece: 1 GiB
 }  // namespace
 
-HeadPlan head_plan(int64_t M, int64_t, int64_t V) {
+HeadPlan head_plan(int64_t M, int64_t V) {
   HeadPlan p{};
   p.large = cdiv(M, GemmLarge::BM) * cdiv(V, GemmLarge::BN) >= 512;
   p.mt = (int)cdiv(M, p.large ? GemmLarge::BM : GemmMedium::BM);
@@ -23,7 +23,9 @@ HeadPlan head_plan(int64_t M, int64_t, int64_t V) {
   const int64_t pieces = cdiv(V, cols);
   p.piece = (int)(pieces <= 1 ? V : cdiv(cdiv(V, pieces), 256) * 256);
   p.pieces = (int)cdiv(V, p.piece);
-  p.refs = (int)cdiv(p.piece, p.large ? GemmLarge::BN : GemmMedium::BN) * 2;
+  const int across = p.large ? GemmLarge::WN : GemmMedium::WN;  // waves that share a row of a tile
+  p.parts = p.runs * across;
+  p.refs = (int)cdiv(p.piece, p.large ? GemmLarge::BN : GemmMedium::BN) * across;
   return p;
 }
 

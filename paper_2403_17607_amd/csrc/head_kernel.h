@@ -23,7 +23,7 @@
 namespace ffmlp {
 
 // f(column within the wave's columns, position in the row's list) for row
-// `row`'s entries among `cols` columns from c0 on, c0 a multiple of 64.
+// `row`'s entries among `cols` columns from c0 on, c0 a multiple of 32.
 template <bool DISTILL, typename F>
 __device__ __forceinline__ void head_hits(const HeadArgs& a, int64_t row, int c0, int cols, F&& f) {
   if (row >= a.M) return;

@@ -69,7 +69,7 @@ struct HeadWs {
 };
 HeadWs head_ws(int64_t M, int64_t D, int64_t V, int top, int mode, bool teacher) {
   HeadWs w{};
-  w.plan = head_plan(M, D, V);
+  w.plan = head_plan(M, V);
   w.keys = (int)(round_up((size_t)V, 256) / kHeadKey) + 1;
   size_t o = 0;
   const auto take = [&](size_t bytes) {
@@ -80,7 +80,7 @@ HeadWs head_ws(int64_t M, int64_t D, int64_t V, int top, int mode, bool teacher)
   w.lse2 = take((size_t)M * 4);
   w.row_loss = take((size_t)M * 4);
   w.alpha = take(4);
-  w.part = take((size_t)w.plan.runs * 2 * M * 8);
+  w.part = take((size_t)w.plan.parts * M * 8);
   w.pick = take((size_t)M * top * 4);
   if (teacher) {
     w.ok = take((size_t)M * 4);
@@ -94,8 +94,8 @@ HeadWs head_ws(int64_t M, int64_t D, int64_t V, int top, int mode, bool teacher)
     w.ref = take((size_t)M * w.plan.refs * 4);
     w.acc = take(w.plan.pieces > 1 ? (size_t)M * D * 4 : 0);
     size_t p = 0;
-    for (int v0 = 0; v0 < V; v0 += w.plan.piece) {  // the last piece may differ
-      const int64_t n = V - v0 < w.plan.piece ? V - v0 : w.plan.piece;
+    const int64_t last = V - (int64_t)(w.plan.pieces - 1) * w.plan.piece;
+    for (const int64_t n : {(int64_t)w.plan.piece, last}) {
       const size_t dh = M > 0 ? gemm_plan(GEMM_DX, M, D, n).partial_bytes : 0, dw = gemm_plan(GEMM_DW, D, n, M).partial_bytes;
       p = p > dh ? p : dh;
       p = p > dw ? p : dw;
@@ -148,7 +148,7 @@ int run_head(bool distill, HeadArgs a, RowLossArgs r, const HeadWs& w, uint8_t* 
     a.chunk = M >= 4096 ? 4096 : 1024;  // few rows: more waves (513 rows, 10007 words: 11 -> 8 us)
   }
   r.partial = a.partial;
-  r.parts = w.plan.runs * 2;
+  r.parts = w.plan.parts;
   r.pick = a.pick;
   r.M = M;
   r.V = V;
