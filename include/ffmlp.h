@@ -357,6 +357,7 @@ int mlp_cross_entropy(const uint16_t* H, int64_t ldh, const uint16_t* W,
  *           twice (its probabilities add up).  A row without an entry (or
  *           with logits of -inf alone) does not count.
  *   logits  [M][top], bf16 or fp32, contiguous.
+ *   temperature  1e-4 .. 1e4.
  * Other arguments as for mlp_cross_entropy. */
 int mlp_distill(const uint16_t* H, int64_t ldh, const uint16_t* W, int64_t ldw,
                 const int64_t* index, const void* logits, int logits_type,

@@ -71,17 +71,18 @@ hipError_t launch_row_loss(const RowLossArgs& a, hipStream_t s);
 hipError_t launch_mean_loss(const RowLossArgs& a, hipStream_t s);
 
 struct HeadPlan {
+  bool rows;                  // head_rows_kernel: whole rows of logits in LDS
   bool large;
   int mt, nt, runs, per_run;  // head_lse_kernel
   int parts;                  // its maxima and sums of a row
   int piece, pieces;          // columns of P, a multiple of 256 unless one piece holds all
   int refs;                   // references of a row in the first piece
 };
-HeadPlan head_plan(int64_t M, int64_t V);
+HeadPlan head_plan(int64_t M, int64_t D, int64_t V);
 
 // The passes over the logits: log-sum-exp; P of the first piece from what that
-// kept, and the losses of the rows (r); P of a later piece.
-enum HeadPass { HEAD_LSE, HEAD_SCALE, HEAD_PROB };
+// kept, and the losses of the rows (r); P of a later piece; all of these at once.
+enum HeadPass { HEAD_LSE, HEAD_SCALE, HEAD_PROB, HEAD_ROWS };
 hipError_t launch_head_ce(HeadPass pass, bool large, const HeadArgs& a, const RowLossArgs& r, hipStream_t s);
 hipError_t launch_head_distill(HeadPass pass, bool large, const HeadArgs& a, const RowLossArgs& r, hipStream_t s);
 
@@ -93,34 +94,28 @@ __device__ __forceinline__ void head_merge(float& m, float& s, float m2, float s
   m = top;
 }
 
-// A row's partial sums merged in a fixed tree by a wave, and its loss.  Returns
-// its lse in base 2 (+inf: the row does not count); `write`: also to memory.
-__device__ __forceinline__ float row_loss(const RowLossArgs& a, int64_t row, int lane, bool write) {
+// A row's loss from its lse in base 2, its target (cross entropy) and the logits
+// (base 2) of its entries, pick(e), by a wave.  Returns the lse, +inf where the row does not count and
+// NaN where it has an index past the vocabulary; `write`: both to memory.
+template <typename F>
+__device__ __forceinline__ float row_end(const RowLossArgs& a, int64_t row, int lane, bool write, float lse, int64_t t, F&& pick) {
   constexpr float kLn2 = 0.69314718f;
-  float m = -__builtin_inff(), s = 0.f;
-  for (int p = lane; p < a.parts; p += 64) {
-    const f32x2 v = a.partial[(int64_t)p * a.M + row];
-    head_merge(m, s, v[0], v[1]);
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) head_merge(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
-  float lse = m + __builtin_amdgcn_logf(s), loss = 0.f;  // logf: base 2
+  float loss = 0.f;
   int state;  // 1 counts, 0 does not, -1 has an index past the vocabulary
   if (a.q) {
     state = a.ok[row];
     if (write) {
       for (int e = lane; e < a.top; e += 64) {
         const float q = a.q[row * a.top + e];
-        if (!(q == 0.f)) loss += q * (kLn2 * (lse - a.pick[row * a.top + e] + __builtin_amdgcn_logf(q)));
+        if (!(q == 0.f)) loss += q * (kLn2 * (lse - pick(e) + __builtin_amdgcn_logf(q)));
       }
 #pragma unroll
       for (int d = 1; d < 64; d *= 2) loss += __shfl_xor(loss, d);
       loss *= a.t2;
     }
   } else {
-    const int64_t t = a.target[row];
     state = t == a.ignore ? 0 : t >= 0 && t < a.V ? 1 : -1;
-    if (state == 1) loss = kLn2 * (lse - a.pick[row]);
+    if (state == 1) loss = kLn2 * (lse - pick(0));
   }
   if (state == 0) {
     lse = __builtin_inff();
@@ -133,6 +128,19 @@ __device__ __forceinline__ float row_loss(const RowLossArgs& a, int64_t row, int
     a.row_loss[row] = loss;
   }
   return lse;
+}
+
+// The same from the row's partial sums, merged in a fixed tree.
+__device__ __forceinline__ float row_loss(const RowLossArgs& a, int64_t row, int lane, bool write) {
+  float m = -__builtin_inff(), s = 0.f;
+  for (int p = lane; p < a.parts; p += 64) {
+    const f32x2 v = a.partial[(int64_t)p * a.M + row];
+    head_merge(m, s, v[0], v[1]);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) head_merge(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
+  return row_end(a, row, lane, write, m + __builtin_amdgcn_logf(s), a.q ? 0 : a.target[row],  // logf: base 2
+                 [&](int e) { return a.pick[row * a.top + e]; });
 }
 #endif
 

@@ -236,11 +236,158 @@ __global__ __launch_bounds__(256) void head_scale_kernel(const HeadArgs a, const
   }
 }
 
+// Few rows and a small vocabulary (the classes of a fused net): a workgroup
+// makes all logits of 16 rows and is done with these rows in one pass: lse, loss
+// and P.  Each of its eight waves has 128 columns and a ring of two slices of
+// W, 32 of k, in LDS of its own, so no wave waits for another until all logits
+// meet in LDS; H's rows are in registers.  Only M / 16 workgroups, and each reads
+// all of W: hence few rows and columns.
+constexpr int kRowsTile = 16, kRowsWaves = 8, kRowsVocab = 128 * kRowsWaves, kRowsDim = 256;
+
+template <bool DISTILL>
+__global__ __launch_bounds__(64 * kRowsWaves) void head_rows_kernel(const HeadArgs a, const RowLossArgs rl) {
+  constexpr int BK = 32, NB = 8, LD = kRowsVocab + 4, ROWS = kRowsTile / kRowsWaves;
+  typedef Side<true, 16 * NB, BK, 64> SW;
+  __shared__ __align__(16) uint8_t lds[kRowsWaves * 2 * SW::BYTES];
+  static_assert(sizeof(lds) >= kRowsTile * LD * 4, "the logits take the place of W's slices");
+  float* logits = reinterpret_cast<float*>(lds);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t m0 = (int64_t)blockIdx.x * kRowsTile;
+  const int nk = (int)((a.D + BK - 1) / BK), col0 = wave * 16 * NB;
+  int64_t target[ROWS] = {};
+  if constexpr (!DISTILL)
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+      if (m0 + r * kRowsWaves + wave < a.M) target[r] = a.target[m0 + r * kRowsWaves + wave];
+  f32x4 acc[NB] = {};
+  if (col0 < a.V) {
+    uint8_t* own = lds + wave * 2 * SW::BYTES;
+    const uint32_t l0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)own;
+    Loader<SW, true, BK, 64> lw;
+    lw.init(a.w, col0, 0, a.D, lane);
+    const auto load = [&](int slot) {  // past D: zeros
+      lw.begin(l0 + slot * SW::BYTES, 0);
+#pragma unroll
+      for (int j = 0; j < SW::PER; ++j) lw.piece(j, lane);
+      lw.end();
+    };
+    u32x4 h[kRowsDim / BK];
+    const int64_t row = m0 + (lane & 15);
+    const uint16_t* hp = a.h.p + (row < a.M ? row : 0) * a.h.ld;
+#pragma unroll
+    for (int k = 0; k < kRowsDim / BK; ++k) {
+      const int c = BK * k + 8 * (lane >> 4);
+      h[k] = load8_bits(hp + c, row < a.M ? (int)a.D - c : 0);
+    }
+    load(0);
+    load(1);
+    // H has arrived before the first step, so no later one waits for it (which
+    // would be for W's newer loads too)
+#pragma unroll
+    for (int k = 0; k < kRowsDim / BK; ++k) asm volatile("" : "+v"(h[k]));
+    Frags<SW, true, NB> fw;
+    fw.init(0, lane);
+    static_for<0, kRowsDim / BK>([&](auto kc) {
+      constexpr int k = decltype(kc)::value;
+      if (k < nk) {
+        uint8_t* s = own + (k & 1) * SW::BYTES;
+        asm volatile("s_waitcnt vmcnt(%0)" :: "n"(SW::PER) : "memory");
+        if (k == nk - 1 && lw.ragged()) {
+          lw.fix(s, BK * k, lane);
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+#pragma unroll
+        for (int n = 0; n < NB; ++n) acc[n] = mfma16(fw.read(s, 0, n), h[k], acc[n]);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slice has been read
+        load(k & 1);
+      }
+    });
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  if (col0 < a.V) {
+    float* o = logits + (lane & 15) * LD + col0 + 4 * (lane >> 4);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) *reinterpret_cast<f32x4*>(o + 16 * n) = acc[n] * a.scale2;
+  }
+  __syncthreads();
+  constexpr int J = kRowsVocab / 512;  // pieces of eight columns of a lane
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    const int64_t row = m0 + r * kRowsWaves + wave, t = target[r];
+    if (row >= a.M) break;
+    float* x = logits + (r * kRowsWaves + wave) * LD;
+    float v[J][8], top = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int c = 512 * j + 8 * lane;
+      lds8(x + c, v[j]);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        v[j][q] = c + q < a.V ? v[j][q] : -__builtin_inff();  // nothing was written past the last tile
+        top = __builtin_fmaxf(top, v[j][q]);
+      }
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) top = __builtin_fmaxf(top, __shfl_xor(top, d));
+    const float at = top == -__builtin_inff() ? 0.f : top;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) sum += __builtin_amdgcn_exp2f(v[j][q] - at);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    const float lse = row_end(rl, row, lane, true, top + __builtin_amdgcn_logf(sum), t, [&](int e) {
+      return x[DISTILL ? a.index[row * a.top + e] : (int)t];
+    });
+    if (a.keep == 0) continue;
+    const bool live = lse != __builtin_inff();  // a row that does not count has none
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[j][q] = live ? __builtin_amdgcn_exp2f(v[j][q] - lse) : 0.f;
+    if constexpr (DISTILL) {
+      // through LDS: a lane takes a run of equal indexes
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        *reinterpret_cast<f32x4*>(x + 512 * j + 8 * lane) = f32x4{v[j][0], v[j][1], v[j][2], v[j][3]};
+        *reinterpret_cast<f32x4*>(x + 512 * j + 8 * lane + 4) = f32x4{v[j][4], v[j][5], v[j][6], v[j][7]};
+      }
+      __builtin_amdgcn_wave_barrier();
+      const int* index = a.index + row * a.top;
+      for (int e = lane; e < a.top; e += 64) {
+        const int c = index[e];
+        if (c >= a.V || (e > 0 && index[e - 1] == c)) continue;  // absent ones are last
+        float w = 0.f;
+        for (int f = e; f < a.top && index[f] == c; ++f) w += a.q[row * a.top + f];
+        x[c] -= w;
+      }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int j = 0; j < J; ++j) lds8(x + 512 * j + 8 * lane, v[j]);
+    } else {
+      if (t != a.ignore)
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+          for (int q = 0; q < 8; ++q) v[j][q] -= t == 512 * j + 8 * lane + q ? 1.f : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int c = 512 * j + 8 * lane;
+      if (c < a.V) *reinterpret_cast<u32x4*>(a.P + row * a.ldp + c) = pack8_bf16(v[j]);
+    }
+  }
+}
+
 template <typename TL, bool DISTILL>
 hipError_t launch_head_tile(HeadPass pass, const HeadArgs& a, const RowLossArgs& r, hipStream_t s) {
   if (pass == HEAD_SCALE) {
     hipLaunchKernelGGL((head_scale_kernel<DISTILL, TL::NB * 16>), dim3((unsigned)((a.M + 3) / 4), (unsigned)((a.keep + a.chunk - 1) / a.chunk)),
                        dim3(256), 0, s, a, r);
+    return hipGetLastError();
+  }
+  if (pass == HEAD_ROWS) {
+    hipLaunchKernelGGL(head_rows_kernel<DISTILL>, dim3((unsigned)((a.M + kRowsTile - 1) / kRowsTile)), dim3(64 * kRowsWaves), 0, s, a, r);
     return hipGetLastError();
   }
   constexpr int lds = gemm_lds_bytes<TL, false, true>();

@@ -69,7 +69,7 @@ struct HeadWs {
 };
 HeadWs head_ws(int64_t M, int64_t D, int64_t V, int top, int mode, bool teacher) {
   HeadWs w{};
-  w.plan = head_plan(M, V);
+  w.plan = head_plan(M, D, V);
   w.keys = (int)(round_up((size_t)V, 256) / kHeadKey) + 1;
   size_t o = 0;
   const auto take = [&](size_t bytes) {
@@ -157,10 +157,12 @@ int run_head(bool distill, HeadArgs a, RowLossArgs r, const HeadWs& w, uint8_t* 
   r.alpha = reinterpret_cast<float*>(ws + w.alpha);
   hipError_t e;
   if (M > 0) {
-    e = launch(HEAD_LSE, w.plan.large, a, r, s);
+    e = launch(w.plan.rows ? HEAD_ROWS : HEAD_LSE, w.plan.large, a, r, s);
     if (e != hipSuccess) return hip_fail(e, "log-sum-exp kernel launch");
-    e = dW ? launch(HEAD_SCALE, w.plan.large, a, r, s) : launch_row_loss(r, s);
-    if (e != hipSuccess) return hip_fail(e, "row loss kernel launch");
+    if (!w.plan.rows) {
+      e = dW ? launch(HEAD_SCALE, w.plan.large, a, r, s) : launch_row_loss(r, s);
+      if (e != hipSuccess) return hip_fail(e, "row loss kernel launch");
+    }
   }
   e = launch_mean_loss(r, s);
   if (e != hipSuccess) return hip_fail(e, "mean loss kernel launch");
@@ -484,7 +486,8 @@ int mlp_distill(const uint16_t* H, int64_t ldh, const uint16_t* W, int64_t ldw, 
   clear_error();
   if (int rc = check_head(H, ldh, W, ldw, dH, dh_type, lddh, dW, dw_type, lddw, loss, row_loss, M, D, V, ws_)) return rc;
   if (top < 1 || top > kHeadMaxTop) return fail(MLP_ERR_INVALID_ARG, "top = %d outside [1, %d]", top, kHeadMaxTop);
-  if (!(temperature > 0.f) || !std::isfinite(temperature)) return fail(MLP_ERR_INVALID_ARG, "temperature must be positive and finite");
+  // its square and inverse, times a logit, stay well within fp32
+  if (!(temperature >= 1e-4f && temperature <= 1e4f)) return fail(MLP_ERR_INVALID_ARG, "temperature outside [1e-4, 1e4]");
   if (!valid_type(logits_type)) return fail(MLP_ERR_UNSUPPORTED, "unknown type of the teacher's logits");
   if (M > 0 && (!index || !logits)) return fail(MLP_ERR_INVALID_ARG, "null index or logits");
   if (!aligned(index, 8) || !aligned(logits, type_size(logits_type))) return fail(MLP_ERR_INVALID_ARG, "misaligned index or logits");

@@ -108,9 +108,10 @@ class _Layer:
     _need = (None, 0)  # the last workspace size asked for, with its arguments
 
     def _ws_bytes(self, *key) -> int:
-        if self._need[0] != key:
-            self._need = (key, self.workspace_bytes(*key))
-        return self._need[1]
+        need = self._need  # read once: other threads may set it
+        if need[0] != key:
+            self._need = need = (key, self.workspace_bytes(*key))
+        return need[1]
 
     def workspace_bytes(self, M: int, mode: int = _base.MLP_MODE_TRAIN) -> int:
         raise NotImplementedError
@@ -320,7 +321,8 @@ class SoftmaxHead(_Layer):
         """Mean over the rows that have an entry of temperature^2
         KL(softmax(logits / temperature) || softmax(H W / temperature)), the
         teacher's distribution over a row's entries alone.  index int64 [M,
-        top] (negative: no entry), logits bf16 or fp32 [M, top]."""
+        top] (negative: no entry), logits bf16 or fp32 [M, top]; temperature
+        from 1e-4 to 1e4."""
         extra, top = self._teacher(index, logits, temperature)
         return self._call(_base.lib().mlp_distill, W, H, extra, top, ws, False, loss, row_loss, None, None, None)
 

@@ -407,6 +407,13 @@ def test_cross_entropy(ffmlp, gpu, M, D, V):
     ce_case(ffmlp, M, D, V, BF, seed=M + V + 1)
 
 
+@pytest.mark.parametrize("M,D,V", [(40, 257, 1024), (65, 264, 7), (4097, 16, 40), (4096, 16, 40), (40, 256, 1025), (17, 255, 1023), (513, 100, 1000)])
+def test_cross_entropy_few_words(ffmlp, gpu, M, D, V):
+    """On either side of what the pass over whole rows takes."""
+    ce_case(ffmlp, M, D, V, BF)
+    distill_case(ffmlp, M, D, V, 5, 1.0, gt=BF, twice=True)
+
+
 @pytest.mark.parametrize("M,D,V", [(2048, 128, 5000), (2050, 64, 4101), (1025, 200, 8192)])
 def test_cross_entropy_large_tiles(ffmlp, gpu, M, D, V):
     ce_case(ffmlp, M, D, V)
@@ -739,5 +746,8 @@ def test_layer_refusals_on_device(ffmlp, gpu):
         he.distill(Wh, X, i3, l3, he.workspace(8, top=3), temperature=0.0)
     with pytest.raises(ffmlp.FFMLPError):
         he.distill(Wh, X, i3, l3, he.workspace(8, top=3), temperature=float("nan"))
+    for out_of_range in (1e-5, 1e5, float("inf"), -1.0):
+        with pytest.raises(ffmlp.FFMLPError, match="temperature"):
+            he.distill(Wh, X, i3, l3, he.workspace(8, top=3), temperature=out_of_range)
     torch.cuda.synchronize()
     assert torch.isfinite(he.cross_entropy(Wh, X, t, wsh)).all()

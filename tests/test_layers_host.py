@@ -69,3 +69,17 @@ def test_workspace_sizes(ffmlp):
     assert h.workspace_bytes(16384, ffmlp.MLP_MODE_INFER) < 64 << 20
     assert h.workspace_bytes(64, top=1024) > h.workspace_bytes(64)
     assert ffmlp.LayerNorm(512).workspace_bytes(100, ffmlp.MLP_MODE_INFER) == 0
+
+
+def test_a_workspace_size_is_that_of_its_own_call(ffmlp):
+    """The remembered size may be replaced by another thread's call at any
+    moment: a call never checks its workspace against that one's."""
+    class Racing(ffmlp.SoftmaxHead):
+        mine, reads = ((8, ffmlp.MLP_MODE_TRAIN, 1), 12345), 0
+
+        @property
+        def _need(self):
+            self.reads += 1
+            return self.mine if self.reads == 1 else ((1, ffmlp.MLP_MODE_INFER, 1), 0)
+
+    assert Racing(16, 32)._ws_bytes(8, ffmlp.MLP_MODE_TRAIN, 1) == 12345
