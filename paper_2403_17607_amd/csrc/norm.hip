@@ -20,31 +20,46 @@ namespace {
 template <bool F32> struct Elem { typedef uint16_t type; };
 template <> struct Elem<true> { typedef float type; };
 
-// Sum over the G consecutive threads that hold a row, in a fixed order: by
-// shuffles, and through LDS (two floats per wave) where they are several waves,
-// which all of the workgroup then passes together.
-template <int G>
-__device__ __forceinline__ void row_sum2(float& a, float& b, float* lds) {
-#pragma unroll
-  for (int m = 1; m < (G < 64 ? G : 64); m *= 2) {
-    a += __shfl_xor(a, m);
-    b += __shfl_xor(b, m);
+// v of the lane whose number differs in bit D, for a v that is the same in all
+// lanes that differ in lower bits only (a butterfly from bit 1 on): on the
+// vector units, without the trip through LDS of a general shuffle.
+template <int D>
+__device__ __forceinline__ float other_half(float v) {
+  const int x = __float_as_int(v);
+  if constexpr (D == 1) return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0xb1, 0xf, 0xf, true));        // quad: 1 0 3 2
+  else if constexpr (D == 2) return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0x4e, 0xf, 0xf, true));   // quad: 2 3 0 1
+  else if constexpr (D == 4) return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true));  // eight lanes mirrored
+  else return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0x140, 0xf, 0xf, true));                        // sixteen mirrored
+}
+template <int LANES, int D = 1>
+__device__ __forceinline__ float lanes_sum(float v) {
+  if constexpr (D >= LANES) return v;
+  else if constexpr (D <= 8) return lanes_sum<LANES, 2 * D>(v + other_half<D>(v));
+  else {
+    const uint32_t x = __float_as_uint(v);
+    const auto s = D == 16 ? __builtin_amdgcn_permlane16_swap(x, x, false, false) : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return lanes_sum<LANES, 2 * D>(__uint_as_float(s[0]) + __uint_as_float(s[1]));
   }
-  if constexpr (G > 64) {
-    const int wave = threadIdx.x >> 6;
-    __syncthreads();  // the last sums have been read
-    if ((threadIdx.x & 63) == 0) {
-      lds[2 * wave] = a;
-      lds[2 * wave + 1] = b;
-    }
-    __syncthreads();
-    a = b = 0.f;
-    const float* of = lds + 2 * (threadIdx.x / G) * (G / 64);
+}
+
+// Sums of K values over the G consecutive threads that hold a row, in a fixed
+// order: within a wave as above, and through LDS (K floats per wave) where they
+// are several waves, which all of the workgroup then passes together.
+template <int G, int K>
+__device__ __forceinline__ void row_sum(float (&v)[K], float* lds) {
 #pragma unroll
-    for (int w = 0; w < G / 64; ++w) {
-      a += of[2 * w];
-      b += of[2 * w + 1];
-    }
+  for (int k = 0; k < K; ++k) v[k] = lanes_sum<(G < 64 ? G : 64)>(v[k]);
+  if constexpr (G > 64) {
+    constexpr int W = G / 64;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    __syncthreads();  // the last sums have been read
+    if (lane == 0)
+#pragma unroll
+      for (int k = 0; k < K; ++k) lds[K * wave + k] = v[k];
+    __syncthreads();
+    const float* of = lds + K * (threadIdx.x / G * W + lane % W);
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = lanes_sum<W>(of[k]);
   }
 }
 
@@ -52,25 +67,24 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, float* lds) {
 template <int G, int J>
 __device__ __forceinline__ void row_stats(const float (&x)[J][8], int lane, int N, float eps, float* lds, float& mean,
                                           float& rstd) {
-  float s = 0.f, z = 0.f;
+  float s[1] = {0.f}, v[1] = {0.f};
 #pragma unroll
   for (int j = 0; j < J; ++j)
 #pragma unroll
-    for (int q = 0; q < 8; ++q) s += x[j][q];
-  row_sum2<G>(s, z, lds);
-  mean = s / (float)N;
-  float v = 0.f;
+    for (int q = 0; q < 8; ++q) s[0] += x[j][q];
+  row_sum<G>(s, lds);
+  mean = s[0] / (float)N;
 #pragma unroll
   for (int j = 0; j < J; ++j) {
     const int n = N - 8 * (j * G + lane);
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
       const float d = x[j][q] - mean;
-      v += q < n ? d * d : 0.f;
+      v[0] += q < n ? d * d : 0.f;
     }
   }
-  row_sum2<G>(v, z, lds);
-  rstd = 1.f / __builtin_sqrtf(v / (float)N + eps);
+  row_sum<G>(v, lds);
+  rstd = 1.f / __builtin_sqrtf(v[0] / (float)N + eps);
 }
 
 // How a row may end: with a whole piece (or, one row to a wave, an even
@@ -293,12 +307,12 @@ __device__ __forceinline__ void bwd_dx(const float (&x)[8], float (&d)[8], const
 
 // Each group of G lanes takes rows blockIdx + k gridDim ... of its own and
 // keeps the sums for dgamma and dbeta of its columns in registers, gamma being
-// in LDS.  bf16 pieces stay packed until they are used; where registers allow
-// (J <= 2), a group asks for its next row before it works on the current one.
+// in LDS.  bf16 pieces stay packed until they are used; where registers allow,
+// a group asks for its next rows (AHEAD of them) before it works on the current one.
 template <int G, int J, int END, bool X32, bool DY32, bool DX32>
 __global__ __launch_bounds__((norm_bwd_threads<G, J>())) void norm_bwd_buf_kernel(const NormArgs a) {
   constexpr int NTHR = norm_bwd_threads<G, J>(), PER = NTHR / G, COLS = 8 * J * G, WPR = G < 64 ? 64 / G : 1;
-  constexpr bool AHEAD = J == 1 || (J == 2 && G <= 64 && !X32 && !DY32);
+  constexpr int AHEAD = J == 1 ? 2 : J == 2 && G <= 64 && !X32 && !DY32 ? 1 : 0, BUFS = AHEAD ? AHEAD : 1;
   __shared__ float lds[32];
   __shared__ __align__(16) float gamma[COLS];
   __shared__ float sums[PER > 1 ? COLS : 1];
@@ -312,58 +326,58 @@ __global__ __launch_bounds__((norm_bwd_threads<G, J>())) void norm_bwd_buf_kerne
   D.init(a.dY, a.lddy, a.N);
   O.init(a.dX, a.lddx, a.N);
   float dg[J][8] = {}, db[J][8] = {};
-  typename BufRows<X32, G, J, END>::Raw nx[J];
-  typename BufRows<DY32, G, J, END>::Raw nd[J];
-  f32x2 nst;
+  struct Row {
+    typename BufRows<X32, G, J, END>::Raw x[J];
+    typename BufRows<DY32, G, J, END>::Raw d[J];
+    f32x2 st;
+  } next[BUFS];
   const int wave_row = G <= 64 ? (int)(threadIdx.x >> 6) * WPR : threadIdx.x / G, in_wave = G < 64 ? (threadIdx.x & 63) / G : 0;
-  const auto fetch = [&](int64_t row0) {
+  const auto fetch = [&](Row& to, int64_t row0) {
     X.at(row0, a.M, a.N);
     D.at(row0, a.M, a.N);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      nx[j] = X.load(j);
-      nd[j] = D.load(j);
+      to.x[j] = X.load(j);
+      to.d[j] = D.load(j);
     }
     const int64_t row = row0 + in_wave;
-    nst = *reinterpret_cast<const f32x2*>(a.stats + 2 * (row < a.M ? row : a.M - 1));
+    to.st = *reinterpret_cast<const f32x2*>(a.stats + 2 * (row < a.M ? row : a.M - 1));
   };
   const int64_t step = (int64_t)gridDim.x * PER;
   int64_t first = (int64_t)blockIdx.x * PER;
-  if (AHEAD) fetch(uniform(first + wave_row));
-  for (; first < a.M; first += step) {
-    const int64_t row0 = uniform(first + wave_row);
-    if (!AHEAD) fetch(row0);
-    typename BufRows<X32, G, J, END>::Raw px[J];
-    typename BufRows<DY32, G, J, END>::Raw pd[J];
+  static_for<0, AHEAD>([&](auto b) { fetch(next[decltype(b)::value], uniform(first + decltype(b)::value * step + wave_row)); });
+  while (first < a.M) {
+    static_for<0, BUFS>([&](auto b) {
+      if (first >= a.M) return;
+      Row& buf = next[decltype(b)::value];
+      const int64_t row0 = uniform(first + wave_row);
+      if (!AHEAD) fetch(buf, row0);
+      const Row now = buf;
+      if (AHEAD) fetch(buf, uniform(first + AHEAD * step + wave_row));
+      float s[2] = {0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      px[j] = nx[j];
-      pd[j] = nd[j];
-    }
-    const f32x2 st = nst;
-    if (AHEAD) fetch(uniform(first + step + wave_row));
-    float s1 = 0.f, s2 = 0.f;
+      for (int j = 0; j < J; ++j) {
+        float g[8], x[8], d[8];
+        lds8(gamma + 8 * (j * G + lane), g);
+        X.widen(j, now.x[j], x);
+        D.widen(j, now.d[j], d);
+        bwd_sums(x, d, g, now.st, dg[j], db[j], s[0], s[1]);
+      }
+      row_sum<G>(s, lds);
+      s[0] /= (float)a.N;
+      s[1] /= (float)a.N;
+      O.at(row0, a.M, a.N);
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      float g[8], x[8], d[8];
-      lds8(gamma + 8 * (j * G + lane), g);
-      X.widen(j, px[j], x);
-      D.widen(j, pd[j], d);
-      bwd_sums(x, d, g, st, dg[j], db[j], s1, s2);
-    }
-    row_sum2<G>(s1, s2, lds);
-    s1 /= (float)a.N;
-    s2 /= (float)a.N;
-    O.at(row0, a.M, a.N);
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      float g[8], x[8], d[8];
-      lds8(gamma + 8 * (j * G + lane), g);
-      X.widen(j, px[j], x);
-      D.widen(j, pd[j], d);
-      bwd_dx(x, d, g, st, s1, s2);
-      O.store(j, d);
-    }
+      for (int j = 0; j < J; ++j) {
+        float g[8], x[8], d[8];
+        lds8(gamma + 8 * (j * G + lane), g);
+        X.widen(j, now.x[j], x);
+        D.widen(j, now.d[j], d);
+        bwd_dx(x, d, g, now.st, s[0], s[1]);
+        O.store(j, d);
+      }
+      first += step;
+    });
   }
   write_part<G, J>(a, dg, db, sums);
 }
@@ -378,25 +392,25 @@ __global__ __launch_bounds__(256) void norm_fwd_long_kernel(const NormArgs a) {
   for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
   const TX* X = static_cast<const TX*>(a.X) + row * a.ldx;
   TY* Y = static_cast<TY*>(a.Y) + row * a.ldy;
-  float s = 0.f, v = 0.f, z = 0.f, x[8];
+  float s[1] = {0.f}, v[1] = {0.f}, x[8];
   for (int c = 8 * threadIdx.x; c < a.N; c += 2048) {
     load8(X + c, a.N - c, x);
     float t = 0.f;
 #pragma unroll
     for (int q = 0; q < 8; ++q) t += x[q];
-    s += t;
+    s[0] += t;
   }
-  row_sum2<256>(s, z, lds);
-  const float mean = s / (float)a.N;
+  row_sum<256>(s, lds);
+  const float mean = s[0] / (float)a.N;
   for (int c = 8 * threadIdx.x; c < a.N; c += 2048) {
     load8(X + c, a.N - c, x);
     float t = 0.f;
 #pragma unroll
     for (int q = 0; q < 8; ++q) t += c + q < a.N ? (x[q] - mean) * (x[q] - mean) : 0.f;
-    v += t;
+    v[0] += t;
   }
-  row_sum2<256>(v, z, lds);
-  const float rstd = 1.f / __builtin_sqrtf(v / (float)a.N + a.eps);
+  row_sum<256>(v, lds);
+  const float rstd = 1.f / __builtin_sqrtf(v[0] / (float)a.N + a.eps);
   if (a.stats && threadIdx.x == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * row) = f32x2{mean, rstd};
   for (int c = 8 * threadIdx.x; c < a.N; c += 2048) {
     const int n = a.N - c;
@@ -424,7 +438,7 @@ __global__ __launch_bounds__(256) void norm_bwd_long_kernel(const NormArgs a) {
   const TX* X = static_cast<const TX*>(a.X) + row * a.ldx;
   const TD* D = static_cast<const TD*>(a.dY) + row * a.lddy;
   const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
-  float s1 = 0.f, s2 = 0.f, x[8], d[8], g[8];
+  float s[2] = {0.f, 0.f}, x[8], d[8], g[8];
   auto load = [&](int c) {
     const int n = a.N - c;
     load8(X + c, n, x);
@@ -444,16 +458,16 @@ __global__ __launch_bounds__(256) void norm_bwd_long_kernel(const NormArgs a) {
       t1 += d[q];
       t2 += d[q] * x[q];
     }
-    s1 += t1;
-    s2 += t2;
+    s[0] += t1;
+    s[1] += t2;
   }
-  row_sum2<256>(s1, s2, lds);
-  s1 /= (float)a.N;
-  s2 /= (float)a.N;
+  row_sum<256>(s, lds);
+  s[0] /= (float)a.N;
+  s[1] /= (float)a.N;
   for (int c = 8 * threadIdx.x; c < a.N; c += 2048) {
     load(c);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) d[q] = st[1] * (d[q] - s1 - x[q] * s2);
+    for (int q = 0; q < 8; ++q) d[q] = st[1] * (d[q] - s[0] - x[q] * s[1]);
     if (a.dx_fp32) store8(static_cast<float*>(a.dX) + row * a.lddx + c, a.N - c, d);
     else store8(static_cast<uint16_t*>(a.dX) + row * a.lddx + c, a.N - c, d);
   }
