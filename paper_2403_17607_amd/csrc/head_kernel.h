@@ -19,6 +19,7 @@
 
 #include "gemm_kernel.h"
 #include "head.h"
+#include "lanes.h"
 
 namespace ffmlp {
 
@@ -106,8 +107,7 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_lse_kernel(const HeadArgs a)
           top = __builtin_fmaxf(top, x);
         }
       // the four lane groups hold the same row
-      top = __builtin_fmaxf(top, __shfl_xor(top, 16));
-      top = __builtin_fmaxf(top, __shfl_xor(top, 32));
+      top = lanes_max<64, 16>(top);
       head_hits<DISTILL>(a, row0 + 16 * m, nw, COLS, [&](int c, int e) {
         if (((c >> 2) & 3) != g) return;
         float x = 0.f;
@@ -152,8 +152,7 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_lse_kernel(const HeadArgs a)
 #pragma unroll
   for (int m = 0; m < TL::MB; ++m) {
     // the lane groups' sums, the maximum being the same
-    sum[m] += __shfl_xor(sum[m], 16);
-    sum[m] += __shfl_xor(sum[m], 32);
+    sum[m] = lanes_sum<64, 16>(sum[m]);
     if (g == 0 && row0 + 16 * m < a.M) part[row0 + 16 * m] = f32x2{mx[m], sum[m]};
   }
 }
@@ -327,15 +326,13 @@ __global__ __launch_bounds__(64 * kRowsWaves) void head_rows_kernel(const HeadAr
         top = __builtin_fmaxf(top, v[j][q]);
       }
     }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) top = __builtin_fmaxf(top, __shfl_xor(top, d));
+    top = lanes_max<64>(top);
     const float at = top == -__builtin_inff() ? 0.f : top;
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
       for (int q = 0; q < 8; ++q) sum += __builtin_amdgcn_exp2f(v[j][q] - at);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    sum = lanes_sum<64>(sum);
     const float lse = row_end(rl, row, lane, true, top + __builtin_amdgcn_logf(sum), t, [&](int e) {
       return x[DISTILL ? a.index[row * a.top + e] : (int)t];
     });

@@ -11,6 +11,7 @@
 // itself, as a second pass over registers.  Sums, statistics and gradients
 // are fp32.
 #include "gemm.h"
+#include "lanes.h"
 #include "rows.h"
 
 namespace ffmlp {
@@ -19,28 +20,6 @@ namespace {
 
 template <bool F32> struct Elem { typedef uint16_t type; };
 template <> struct Elem<true> { typedef float type; };
-
-// v of the lane whose number differs in bit D, for a v that is the same in all
-// lanes that differ in lower bits only (a butterfly from bit 1 on): on the
-// vector units, without the trip through LDS of a general shuffle.
-template <int D>
-__device__ __forceinline__ float other_half(float v) {
-  const int x = __float_as_int(v);
-  if constexpr (D == 1) return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0xb1, 0xf, 0xf, true));        // quad: 1 0 3 2
-  else if constexpr (D == 2) return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0x4e, 0xf, 0xf, true));   // quad: 2 3 0 1
-  else if constexpr (D == 4) return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true));  // eight lanes mirrored
-  else return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0x140, 0xf, 0xf, true));                        // sixteen mirrored
-}
-template <int LANES, int D = 1>
-__device__ __forceinline__ float lanes_sum(float v) {
-  if constexpr (D >= LANES) return v;
-  else if constexpr (D <= 8) return lanes_sum<LANES, 2 * D>(v + other_half<D>(v));
-  else {
-    const uint32_t x = __float_as_uint(v);
-    const auto s = D == 16 ? __builtin_amdgcn_permlane16_swap(x, x, false, false) : __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return lanes_sum<LANES, 2 * D>(__uint_as_float(s[0]) + __uint_as_float(s[1]));
-  }
-}
 
 // Sums of K values over the G consecutive threads that hold a row, in a fixed
 // order: within a wave as above, and through LDS (K floats per wave) where they
@@ -533,7 +512,7 @@ hipError_t by_types(bool a32, bool b32, F&& f) {
 template <typename F>
 bool by_row_forward(int N, F&& f) {
   FFMLP_ROW(8, 1) FFMLP_ROW(16, 1) FFMLP_ROW(32, 1) FFMLP_ROW(64, 1) FFMLP_ROW(64, 2) FFMLP_ROW(256, 1)
-  FFMLP_ROW(512, 1) FFMLP_ROW(256, 4) FFMLP_ROW(512, 4)
+  FFMLP_ROW(512, 1) FFMLP_ROW(512, 2) FFMLP_ROW(512, 4)
   return false;
 }
 template <typename F>
