@@ -38,7 +38,7 @@ struct GemmArgs {
   float* partial;  // [splits][M][N] fp32 when splits > 1
   int splits;
   int64_t kper;    // k of a split, a multiple of the tile's BK
-  int tiles, mt, nt;
+  int mt, nt;
 };
 
 // Workgroup tiles (gemm_kernel.h) and which sides have k across their rows.

@@ -115,7 +115,6 @@ hipError_t launch_gemm(int form, GemmArgs a, float* partial, hipStream_t s) {
   const GemmPlan p = gemm_plan(form, a.M, a.N, a.K);
   a.mt = p.mt;
   a.nt = p.nt;
-  a.tiles = p.mt * p.nt;
   a.splits = p.splits;
   a.kper = p.kper;
   a.partial = partial;

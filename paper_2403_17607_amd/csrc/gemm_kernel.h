@@ -303,13 +303,17 @@ __device__ __forceinline__ void out_rows(uint8_t* lds, f32x4 (&acc)[TL::MB][TL::
   });
 }
 
-// Tile `t` of mt x nt, in an order that keeps a chiplet's tiles together: the
-// hardware deals workgroups out to the eight chiplets in turn, each with its
-// own L2, so workgroup b takes tile (b % 8) of eight equal runs; within the
-// order, groups of eight tile rows share the n side's tiles.
-__device__ __forceinline__ void gemm_tile_of(int b, int mt, int nt, int& tm, int& tn) {
-  const int total = mt * nt, q = total / 8, r = total % 8, x = b % 8, y = b / 8;
-  const int t = x * q + (x < r ? x : r) + y;
+// The tile and the split of workgroup b of mt x nt tiles, `splits` each, in an
+// order that keeps a chiplet's tiles together: the hardware deals workgroups out
+// to the eight chiplets in turn, each with its own L2, so workgroup b takes item
+// (b % 8) of eight equal runs.  A run stays within a split as far as it can (k is
+// then shared by its tiles), and within the order, groups of eight tile rows
+// share the n side's tiles.
+__device__ __forceinline__ void gemm_tile_of(int b, int mt, int nt, int splits, int& tm, int& tn, int& split) {
+  const int tiles = mt * nt, total = tiles * splits, q = total / 8, r = total % 8, x = b % 8, y = b / 8;
+  int t = x * q + (x < r ? x : r) + y;
+  split = t / tiles;
+  t -= split * tiles;
   constexpr int G = 8;
   const int per = G * nt, grp = t / per, first = grp * G;
   const int rows = mt - first < G ? mt - first : G;
@@ -414,9 +418,8 @@ __device__ __forceinline__ void out8(const GemmOut& o, int64_t m, int n, int N, 
 template <typename TL, bool MT, bool NT>
 __global__ __launch_bounds__(TL::NTHR, 2) void gemm_kernel(const GemmArgs a) {
   extern __shared__ __align__(16) uint8_t gemm_lds[];
-  const int b = blockIdx.x % a.tiles, split = blockIdx.x / a.tiles;
-  int tm, tn;
-  gemm_tile_of(b, a.mt, a.nt, tm, tn);
+  int tm, tn, split;
+  gemm_tile_of(blockIdx.x, a.mt, a.nt, a.splits, tm, tn, split);
   const int64_t m0 = (int64_t)tm * TL::BM;
   const int n0 = tn * TL::BN;
   const int64_t k0 = split * a.kper, k1 = k0 + a.kper < a.K ? k0 + a.kper : a.K;
@@ -456,7 +459,7 @@ hipError_t launch_gemm_tile(GemmArgs a, hipStream_t s) {
   int occ;
   const hipError_t e = kernel_occupancy(reinterpret_cast<const void*>(k), TL::NTHR, lds, &occ);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k, dim3((unsigned)(a.tiles * a.splits)), dim3(TL::NTHR), lds, s, a);
+  hipLaunchKernelGGL(k, dim3((unsigned)(a.mt * a.nt * a.splits)), dim3(TL::NTHR), lds, s, a);
   return hipGetLastError();
 }
 

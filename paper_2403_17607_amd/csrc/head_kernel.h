@@ -41,13 +41,6 @@ __device__ __forceinline__ void head_hits(const HeadArgs& a, int64_t row, int c0
   }
 }
 
-// Row tile and run of a workgroup: a chiplet (blockIdx % 8) gets neighbouring
-// row tiles with all their runs, so that its L2 holds its rows of H.
-__device__ __forceinline__ int head_block(int b, int total) {
-  const int q = total / 8, r = total % 8, x = b % 8, y = b / 8;
-  return x * q + (x < r ? x : r) + y;
-}
-
 // eight results of a row as fp16 (E) or bf16 (P)
 __device__ __forceinline__ u32x4 pack8_f16(const float* p) {
   u32x4 u;
@@ -65,8 +58,8 @@ __device__ __forceinline__ u32x4 pack8_bf16(const float* p) {
 template <typename TL, bool DISTILL>
 __global__ __launch_bounds__(TL::NTHR, 2) void head_lse_kernel(const HeadArgs a) {
   extern __shared__ __align__(16) uint8_t head_lds[];
-  const int t = head_block(blockIdx.x, a.mt * a.runs);
-  const int tm = t / a.runs, run = t % a.runs;
+  int tm, run, one;
+  gemm_tile_of(blockIdx.x, a.mt, a.runs, 1, tm, run, one);
   const int64_t m0 = (int64_t)tm * TL::BM;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   constexpr int COLS = TL::NB * 16;
@@ -161,8 +154,8 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_lse_kernel(const HeadArgs a)
 template <typename TL, bool DISTILL>
 __global__ __launch_bounds__(TL::NTHR, 2) void head_prob_kernel(const HeadArgs a) {
   extern __shared__ __align__(16) uint8_t head_lds[];
-  int tm, tn;
-  gemm_tile_of(blockIdx.x, a.mt, a.nt, tm, tn);
+  int tm, tn, one;
+  gemm_tile_of(blockIdx.x, a.mt, a.nt, 1, tm, tn, one);
   const int64_t m0 = (int64_t)tm * TL::BM;
   const int n0 = tn * TL::BN;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
