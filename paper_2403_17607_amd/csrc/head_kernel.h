@@ -41,15 +41,11 @@ __device__ __forceinline__ void head_hits(const HeadArgs& a, int64_t row, int c0
   }
 }
 
-// eight results of a row as fp16 (E) or bf16 (P)
-__device__ __forceinline__ u32x4 pack8_f16(const float* p) {
-  u32x4 u;
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-    u[q] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)p[2 * q], (_Float16)p[2 * q + 1]});
-  }
-  return u;
+// four results as fp16 (E), eight as bf16 (P)
+__device__ __forceinline__ u32x2 pack4_f16(const f32x4& p) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  return u32x2{__builtin_bit_cast(uint32_t, f16x2{(_Float16)p[0], (_Float16)p[1]}),
+               __builtin_bit_cast(uint32_t, f16x2{(_Float16)p[2], (_Float16)p[3]})};
 }
 __device__ __forceinline__ u32x4 pack8_bf16(const float* p) {
   return u32x4{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])};
@@ -86,7 +82,8 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_lse_kernel(const HeadArgs a)
     const int g = ln >> 4;
     const int64_t row0 = mw + (ln & 15);
     const bool keep = a.keep > n0;
-    float* part = reinterpret_cast<float*>(head_lds) + wave * 16 * OutTile<TL>::LD;
+    constexpr int LDE = COLS + 8;  // fp16: eight lanes write eight rows to different banks
+    uint16_t* part = reinterpret_cast<uint16_t*>(head_lds) + wave * 16 * LDE;
     static_for<0, TL::MB>([&](auto mc) {
       constexpr int m = decltype(mc)::value;
       float top = -__builtin_inff();
@@ -94,13 +91,11 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_lse_kernel(const HeadArgs a)
       for (int n = 0; n < TL::NB; ++n)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          float x = acc[m][n][q] * a.scale2;
-          if (n0 + TL::BN > a.V) x = nw + 16 * n + 4 * g + q < a.V ? x : -__builtin_inff();
-          acc[m][n][q] = x;
-          top = __builtin_fmaxf(top, x);
+          if (n0 + TL::BN > a.V) acc[m][n][q] = nw + 16 * n + 4 * g + q < a.V ? acc[m][n][q] : -__builtin_inff();
+          top = __builtin_fmaxf(top, acc[m][n][q]);
         }
       // the four lane groups hold the same row
-      top = lanes_max<64, 16>(top);
+      top = lanes_max<64, 16>(top) * a.scale2;
       head_hits<DISTILL>(a, row0 + 16 * m, nw, COLS, [&](int c, int e) {
         if (((c >> 2) & 3) != g) return;
         float x = 0.f;
@@ -108,7 +103,7 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_lse_kernel(const HeadArgs a)
         for (int n = 0; n < TL::NB; ++n)
 #pragma unroll
           for (int q = 0; q < 4; ++q) x = (c >> 4) == n && (c & 3) == q ? acc[m][n][q] : x;
-        a.pick[(row0 + 16 * m) * a.top + e] = x;
+        a.pick[(row0 + 16 * m) * a.top + e] = x * a.scale2;
       });
       // a sum of 2^(x - at), its largest term 2^15
       const float at = top == -__builtin_inff() ? 0.f : top - 15.f;
@@ -117,22 +112,23 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_lse_kernel(const HeadArgs a)
       for (int n = 0; n < TL::NB; ++n)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          acc[m][n][q] = __builtin_amdgcn_exp2f(acc[m][n][q] - at);
+          acc[m][n][q] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[m][n][q], a.scale2, -at));
           s += acc[m][n][q];
         }
       head_merge(mx[m], sum[m], top == -__builtin_inff() ? top : at, s);
       if (keep) {
         if (g == 0 && row0 + 16 * m < a.M) a.ref[(int64_t)(nw / COLS) * a.M + row0 + 16 * m] = at;
-        constexpr int LD = OutTile<TL>::LD, LPR = COLS / 8, RPI = 64 / LPR;
+        constexpr int LPR = COLS / 8, RPI = 64 / LPR;
 #pragma unroll
-        for (int n = 0; n < TL::NB; ++n) *reinterpret_cast<f32x4*>(part + (ln & 15) * LD + 16 * n + 4 * g) = acc[m][n];
+        for (int n = 0; n < TL::NB; ++n)
+          *reinterpret_cast<u32x2*>(part + (ln & 15) * LDE + 16 * n + 4 * g) = pack4_f16(acc[m][n]);
         __builtin_amdgcn_wave_barrier();
         const int c = nw + 8 * (ln % LPR);
-#pragma unroll 1
+#pragma unroll
         for (int r = ln / LPR; r < 16; r += RPI) {
           const int64_t row = mw + 16 * m + r;
           if (c < a.keep && row < a.M)
-            *reinterpret_cast<u32x4*>(a.P + row * a.ldp + c) = pack8_f16(part + r * LD + 8 * (ln % LPR));
+            *reinterpret_cast<u32x4*>(a.P + row * a.ldp + c) = *reinterpret_cast<const u32x4*>(part + r * LDE + 8 * (ln % LPR));
         }
         __builtin_amdgcn_wave_barrier();
       }
