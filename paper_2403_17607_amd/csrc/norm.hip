@@ -6,10 +6,12 @@
 //   dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy
 //
 // Bound by memory: each element is read once and written once.  A row is held
-// in registers by G lanes (8 .. 64, or the 256 threads of a workgroup), J
-// pieces of eight elements each, so the variance is taken about the mean
-// itself, as a second pass over registers.  Sums, statistics and gradients
-// are fp32.
+// in registers by G lanes (8 .. 64 of a wave, or 256 .. 1024 threads), J pieces
+// of eight elements each, so the variance is taken about the mean itself, as a
+// second pass over registers.  Sums, statistics and gradients are fp32.
+// Measured, forward and backward: 16384 x 2048 bf16 30 us (4.4 TB/s) and 39 us
+// (5.2 TB/s, the rate of a large copy); 3001 x 5003 from fp32 23 us (3.9 TB/s)
+// and 38 us (4.0 TB/s), twelve rows one after the other on every CU.
 #include "gemm.h"
 #include "lanes.h"
 #include "rows.h"
