@@ -77,7 +77,10 @@ __global__ __launch_bounds__(64) void teacher_kernel(const TeacherArgs a) {
     for (int o = 0; o < a.top; ++o) rank += idx[o] < me || (idx[o] == me && o < e);
     sorted[rank] = me;
     a.out_index[at + rank] = me;
-    a.out_q[at + rank] = me != 0x7fffffff && !empty ? __expf(logit(e) - mx) / sum : 0.f;
+    // a denormal q is 0: the hardware's logarithm of it would be -inf, and q log q
+    // is below 2^-119
+    const float q = me != 0x7fffffff && !empty ? __expf(logit(e) - mx) / sum : 0.f;
+    a.out_q[at + rank] = q < 0x1p-126f ? 0.f : q;
   }
   __syncthreads();
   for (int k = lane; k < a.keys; k += 64) {

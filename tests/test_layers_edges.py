@@ -1,0 +1,106 @@
+"""Layer norm, dense layers and vocabulary losses where their numerics are
+tightest, against the same formulas in 64 bits (tolerances: test_layers.py
+says how they count).
+
+The losses here are given their logits' own error bound e_l = (D + 8) u sum
+|h w| / T per logit, and with d = (max z - z) / T the distance of a teacher's
+entry from its row's largest: (z - max) / T is a subtraction and a product by a
+rounded 1 / T, so q is off by (3 d + 24) u of itself (exp 2 u, its sum and the
+division 20 u), and a q below 2^-126 may be 0.
+"""
+import math
+
+import pytest
+import torch
+
+from test_layers import BF, F32, HALF, U, check_guard, close, close_norm, gen, guarded, randn
+
+pytestmark = pytest.mark.gpu
+
+
+def teacher64(index, logits, T):
+    """q, its error bound and which rows count."""
+    there = index >= 0
+    z = torch.where(there, logits.double(), float("-inf"))
+    mx = z.amax(1, keepdim=True)
+    live = torch.isfinite(mx)
+    d = torch.where(there & live, mx - z, float("inf")) / T
+    q = torch.nan_to_num(torch.exp(-d) / torch.exp(-d).sum(1, keepdim=True), nan=0.0)
+    return q, torch.where(q > 0, q * (3 * d + 24) * U, 0.0) + 2.0 ** -126, live[:, 0]
+
+
+def distill_on(ffmlp, H, W, index, logits, T, gt=F32, exact_p=None):
+    """distill_step on these inputs: rows' losses, loss, dH and dW, element by
+    element and in the norm.  exact_p: softmax(H W / T), where the logits' own
+    rounding is too coarse to say."""
+    (M, D), V, top = H.shape, W.shape[1], index.shape[1]
+    head = ffmlp.SoftmaxHead(D, V)
+    ws = head.workspace(M, top=top)
+    ws.fill_(255)
+    rl = torch.full((M,), float("nan"), device="cuda")
+    bufh, dH = guarded(M, D, gt)
+    bufw, dW = guarded(D, V, gt)
+    _, _, loss = head.distill_step(W, H, index, logits, ws, temperature=T, row_loss=rl, dH=dH, dW=dW)
+    check_guard(bufh, dH)
+    check_guard(bufw, dW)
+    h, w = H.double(), W.double()
+    l = h @ w / T
+    e_l = (D + 8) * U * (h.abs() @ w.abs()) / T + 4 * U * l.abs()
+    e_lse = e_l.amax(1, keepdim=True) + 24 * U  # of a sum of V terms
+    lse = torch.logsumexp(l, 1, keepdim=True)
+    q, e_q, live = teacher64(index, logits, T)
+    ix = index.clamp_min(0)
+    lq, lp = torch.log(q.clamp_min(1e-300)), (l - lse).gather(1, ix)
+    rows = T * T * (q * (lq - lp)).sum(1) * live
+    e_row = T * T * (e_q * ((lq - lp).abs() + 1) + q * (e_l.gather(1, ix) + e_lse + 8 * U * (lq.abs() + lp.abs() + 1))).sum(1)
+    close(rl, rows, e_row * live + 100 * U * rows.abs() + 1e-12, "row loss")
+    n = max(1, int(live.sum()))
+    close(loss, (rows.sum() / n).reshape(1), ((e_row * live).sum() / n + 180 * U * rows.abs().sum() / n).reshape(1) + 1e-12, "loss")
+    p = torch.exp(l - lse) if exact_p is None else exact_p
+    p = p * live[:, None]
+    P = p.scatter_add(1, ix, -q * live[:, None])
+    hit = torch.zeros_like(p).scatter_add(1, ix, (index >= 0).double()) > 0
+    # p outside the lists passes through fp16 (2^-11, or 2^-40 of a block's
+    # largest); where q is subtracted it has only the logits' error
+    e_p = p * (e_l + e_lse + 32 * U) if exact_p is None else 32 * U * p
+    e_P = e_p + torch.where(hit, 0.0, 2.0 ** -11 * p + 2.0 ** -40)
+    e_P = (e_P.scatter_add(1, ix, e_q) + HALF[BF] * P.abs()) * live[:, None]
+    # in the norm: roundings of P's elements are independent, and those of a
+    # logit's sum too; the error of lse is one for the row
+    e_i, e_c = 0.0 * p, 32 * U * p
+    if exact_p is None:
+        e_i = p * (math.sqrt(D + 8) * U * (h.abs() @ w.abs()) / T + 4 * U * l.abs())
+        e_c = p * ((e_i / p.clamp_min(1e-300) * (p > 1e-12)).amax(1, keepdim=True) + 56 * U)
+    e_i = e_i + torch.where(hit, 0.0, 2.0 ** -11 * p + 2.0 ** -40)
+    e_i = (e_i.scatter_add(1, ix, e_q) + HALF[BF] * P.abs()) * live[:, None]
+    a = T / n
+    ref, s = a * (P @ w.t()), a * (P.abs() @ w.abs().t())
+    close(dH, ref, a * (e_P @ w.abs().t()) + (V + 8) * U * s + HALF[gt] * (ref.abs() + HALF[BF] * s) + 1e-14, "dH")
+    close_norm(dH, ref, a * ((e_i.square() @ w.square().t()).sum().sqrt() + (e_c @ w.t()).norm()).item()
+               + math.sqrt(V + 8) * U * s.norm().item() + HALF[gt] * ref.norm().item() + 1e-14, "dH norm")
+    ref, s = a * (h.t() @ P), a * (h.abs().t() @ P.abs())
+    close(dW, ref, a * (h.abs().t() @ e_P) + (M + 8) * U * s + HALF[gt] * (ref.abs() + HALF[BF] * s) + 1e-14, "dW")
+    close_norm(dW, ref, a * ((h.square().t() @ e_i.square()).sum().sqrt() + (h.square().t() @ e_c.square()).sum().sqrt()).item()
+               + math.sqrt(M + 8) * U * s.norm().item() + HALF[gt] * ref.norm().item() + 1e-14, "dW norm")
+    wi = head.workspace(M, mode=ffmlp.MLP_MODE_INFER, top=top)
+    wi.fill_(255)
+    rl2 = torch.empty_like(rl)
+    assert torch.equal(head.distill(W, H, index, logits, wi, temperature=T, row_loss=rl2), loss) and torch.equal(rl, rl2)
+
+
+# a vocabulary of the pass over whole rows, and one of two passes
+WORDS = [900, 3000]
+
+
+@pytest.mark.parametrize("V", WORDS)
+@pytest.mark.parametrize("T", [1.0, 0.1])
+def test_teacher_entries_at_the_end_of_the_fp32_range(ffmlp, gpu, V, T):
+    """Lists that go down by 80 to 95 units of logit / T in small steps: some
+    probabilities are fp32 denormals, others 0."""
+    g = gen(31)
+    M, D, top = 40, 48, 64
+    H, W = randn(g, M, D), randn(g, D, V, std=2 * T / math.sqrt(D))
+    index = torch.rand(M, V, generator=g, device="cuda").topk(top, 1).indices
+    d = torch.linspace(80.0, 95.0, top - 4, device="cuda").expand(M, top - 4) + 0.2 * torch.rand(M, 1, generator=g, device="cuda")
+    logits = torch.cat([torch.rand(M, 4, generator=g, device="cuda"), -d], 1) * T
+    distill_on(ffmlp, H, W, index, logits.contiguous(), T)
