@@ -43,9 +43,8 @@ __global__ __launch_bounds__(64) void teacher_kernel(const TeacherArgs a) {
   const int lane = threadIdx.x;
   const int64_t at = row * a.top;
   auto logit = [&](int e) {
-    const float z = a.logits_fp32 ? static_cast<const float*>(a.logits)[at + e]
-                                  : __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.logits)[at + e] << 16);
-    return z * a.inv_t;
+    return a.logits_fp32 ? static_cast<const float*>(a.logits)[at + e]
+                         : __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.logits)[at + e] << 16);
   };
   float mx = -__builtin_inff();
   int bad = 0;
@@ -65,9 +64,11 @@ __global__ __launch_bounds__(64) void teacher_kernel(const TeacherArgs a) {
     bad |= __shfl_xor(bad, d);
   }
   const bool empty = mx == -__builtin_inff();
+  // divided by T after the subtraction: a type's lowest value stays finite
+  auto weight = [&](int e) { return __expf((logit(e) - mx) * a.inv_t); };
   float sum = 0.f;
   for (int e = lane; e < a.top; e += 64)
-    if (a.index[at + e] >= 0 && !empty) sum += __expf(logit(e) - mx);
+    if (a.index[at + e] >= 0 && !empty) sum += weight(e);
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
   __syncthreads();
@@ -79,7 +80,7 @@ __global__ __launch_bounds__(64) void teacher_kernel(const TeacherArgs a) {
     a.out_index[at + rank] = me;
     // a denormal q is 0: the hardware's logarithm of it would be -inf, and q log q
     // is below 2^-119
-    const float q = me != 0x7fffffff && !empty ? __expf(logit(e) - mx) / sum : 0.f;
+    const float q = me != 0x7fffffff && !empty ? weight(e) / sum : 0.f;
     a.out_q[at + rank] = q < 0x1p-126f ? 0.f : q;
   }
   __syncthreads();

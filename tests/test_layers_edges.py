@@ -104,3 +104,24 @@ def test_teacher_entries_at_the_end_of_the_fp32_range(ffmlp, gpu, V, T):
     d = torch.linspace(80.0, 95.0, top - 4, device="cuda").expand(M, top - 4) + 0.2 * torch.rand(M, 1, generator=g, device="cuda")
     logits = torch.cat([torch.rand(M, 4, generator=g, device="cuda"), -d], 1) * T
     distill_on(ffmlp, H, W, index, logits.contiguous(), T)
+
+
+@pytest.mark.parametrize("V", WORDS)
+@pytest.mark.parametrize("zt", [BF, F32])
+@pytest.mark.parametrize("T", [0.25, 0.5])
+def test_teacher_logits_of_the_lowest_value(ffmlp, gpu, V, zt, T):
+    """Lists masked with the type's lowest value, alone (all entries alike),
+    beside ordinary logits, and beside the largest value."""
+    g = gen(32)
+    M, D, top = 33, 40, 6
+    H, W = randn(g, M, D), randn(g, D, V, std=2 * T / math.sqrt(D))
+    index = torch.rand(M, V, generator=g, device="cuda").topk(top, 1).indices
+    logits = torch.randn(M, top, generator=g, device="cuda").to(zt)
+    lowest = torch.finfo(zt).min
+    logits[0] = lowest
+    logits[1, :3] = lowest
+    logits[2], logits[2, 4] = lowest, float("-inf")
+    logits[3] = -lowest
+    logits[4, 0], logits[4, 1] = lowest, -lowest
+    logits[5] = float("-inf")  # does not count
+    distill_on(ffmlp, H, W, index, logits, T)
