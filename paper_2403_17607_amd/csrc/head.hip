@@ -117,7 +117,7 @@ __global__ __launch_bounds__(1024) void mean_loss_kernel(const RowLossArgs a) {
   int n = 0;
   for (int64_t r = t; r < a.M; r += 1024) {
     s += a.row_loss[r];
-    n += a.lse2[r] != __builtin_inff();
+    n += a.lse[r][1] != __builtin_inff();
   }
   sums[t] = s;
   counts[t] = n;

@@ -1,16 +1,20 @@
 // Losses of the logits H W over a vocabulary, never stored whole.
 //
-//   x = log2(e) / T * (H W)                    (the logits in base-2 units)
-//   lse = log2 sum_v 2^x
-//   P = 2^(x - lse) - q                        (q: the target distribution)
+//   x = H W,  c = log2(e) / T                  (logits / T in base 2: x c)
+//   m = max_v x,  ls = log2 sum_v 2^((x - m) c)
+//   P = 2^((x - m) c - ls) - q                 (q: the target distribution)
+//
+// Products are subtracted before they are scaled: x c and m c themselves, at
+// |x c| beyond 2^24, are rounded to whole numbers and more, and an exponent that
+// is off by that much overflowed the fp16 below.
 //
 // head_lse_kernel walks a run of column tiles with one row tile and keeps the
 // running maximum and sum of every row in registers, so the logits live only
 // in the matrix cores' results.  The gradients dH = P W^T and dW = H^T P take P
 // as bf16, a piece of the vocabulary at a time.  For the first piece the same
-// pass stores 2^(x - r) as fp16, r + 15 the maximum of the row's columns in a
-// wave's tile, and head_scale_kernel turns that into P in place once lse is
-// known.  fp16 up to 2^15: its rounding (2^-12 relative, at most 2^-40 of a
+// pass stores 2^((x - r) c + 15) as fp16, r the largest product of the row's
+// columns in a wave's tile, and head_scale_kernel turns that into P in place once
+// m and ls are known.  fp16 up to 2^15: its rounding (2^-12 relative, at most 2^-40 of a
 // probability in absolute terms) does not add to that of P (2^-9).  The logits
 // of later pieces are recomputed by head_prob_kernel.  q is sparse:
 // the one target of a row, or the teacher's top entries sorted by index, with
@@ -104,7 +108,7 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_lse_kernel(const HeadArgs a)
           top = __builtin_fmaxf(top, acc[m][n][q]);
         }
       // the four lane groups hold the same row
-      top = lanes_max<64, 16>(top) * a.scale2;
+      top = lanes_max<64, 16>(top);
       head_hits<DISTILL>(a, row0 + 16 * m, nw, COLS, [&](int c, int e) {
         if (((c >> 2) & 3) != g) return;
         float x = 0.f;
@@ -112,21 +116,21 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_lse_kernel(const HeadArgs a)
         for (int n = 0; n < TL::NB; ++n)
 #pragma unroll
           for (int q = 0; q < 4; ++q) x = (c >> 4) == n && (c & 3) == q ? acc[m][n][q] : x;
-        a.pick[(row0 + 16 * m) * a.top + e] = x * a.scale2;
+        a.pick[(row0 + 16 * m) * a.top + e] = x;
       });
-      // a sum of 2^(x - at), its largest term 2^15
-      const float at = top == -__builtin_inff() ? 0.f : top - 15.f;
+      // a sum of 2^((x - top) c + 15), its largest term 2^15 exactly
+      const float at = top == -__builtin_inff() ? 0.f : top;
       float s = 0.f;
 #pragma unroll
       for (int n = 0; n < TL::NB; ++n)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          acc[m][n][q] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[m][n][q], a.scale2, -at));
+          acc[m][n][q] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[m][n][q] - at, a.scale2, 15.f));
           s += acc[m][n][q];
         }
-      head_merge(mx[m], sum[m], top == -__builtin_inff() ? top : at, s);
+      head_merge(mx[m], sum[m], top, s, a.scale2);
       if (keep) {
-        if (g == 0 && row0 + 16 * m < a.M) a.ref[(int64_t)(nw / COLS) * a.M + row0 + 16 * m] = at;
+        if (g == 0 && row0 + 16 * m < a.M) a.ref[(int64_t)(nw / COLS) * a.M + row0 + 16 * m] = top;
         constexpr int LPR = COLS / 8, RPI = 64 / LPR;
 #pragma unroll
         for (int n = 0; n < TL::NB; ++n)
@@ -151,7 +155,7 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_lse_kernel(const HeadArgs a)
   for (int m = 0; m < TL::MB; ++m) {
     // the lane groups' sums, the maximum being the same
     sum[m] = lanes_sum<64, 16>(sum[m]);
-    if (g == 0 && row0 + 16 * m < a.M) part[row0 + 16 * m] = f32x2{mx[m], sum[m]};
+    if (g == 0 && row0 + 16 * m < a.M) part[row0 + 16 * m] = f32x2{mx[m], sum[m] * 0x1p-15f};
   }
 }
 
@@ -178,13 +182,14 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_prob_kernel(const HeadArgs a
   out_rows<TL>(head_lds, acc, [&](auto mc) {
     constexpr int m = decltype(mc)::value;
     const int64_t row = row0 + 16 * m;
-    const float lse = row < a.M ? a.lse2[row] : __builtin_inff();
-    const bool live = lse != __builtin_inff();  // a row that does not count has none
+    RowLse lse = {0.f, __builtin_inff()};
+    if (row < a.M) lse = RowLse{a.lse[row][0], a.lse[row][1]};
+    const bool live = lse.live();  // a row that does not count has none
 #pragma unroll
     for (int n = 0; n < TL::NB; ++n)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        acc[m][n][q] = live ? __builtin_amdgcn_exp2f(acc[m][n][q] * a.scale2 - lse) : 0.f;
+        acc[m][n][q] = live ? __builtin_amdgcn_exp2f(lse.log2_p(acc[m][n][q], a.scale2)) : 0.f;
     head_hits<DISTILL>(a, row, a.col0 + nw, COLS, [&](int c, int e) {
       if (((c >> 2) & 3) != g) return;
       const float w = DISTILL ? a.q[row * a.top + e] : 1.f;
@@ -208,8 +213,8 @@ __global__ __launch_bounds__(256) void head_scale_kernel(const HeadArgs a, const
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= a.M) return;
   const int lane = threadIdx.x & 63;
-  const float lse = row_loss(rl, row, lane, blockIdx.y == 0);
-  const bool live = lse != __builtin_inff();
+  const RowLse lse = row_loss(rl, row, lane, blockIdx.y == 0);
+  const bool live = lse.live();
   const int c1 = (int)(blockIdx.y + 1) * a.chunk < a.keep ? (int)(blockIdx.y + 1) * a.chunk : a.keep;
 #pragma unroll 2
   for (int c0 = blockIdx.y * a.chunk; c0 < c1; c0 += 512) {
@@ -217,7 +222,7 @@ __global__ __launch_bounds__(256) void head_scale_kernel(const HeadArgs a, const
     if (c >= c1) continue;
     uint16_t* p = a.P + row * a.ldp + c;
     const u32x4 u = *reinterpret_cast<const u32x4*>(p);
-    const float f = live ? __builtin_amdgcn_exp2f(a.ref[(int64_t)(c / G) * a.M + row] - lse) : 0.f;
+    const float f = live ? __builtin_amdgcn_exp2f(lse.log2_p(a.ref[(int64_t)(c / G) * a.M + row], a.scale2) - 15.f) : 0.f;
     float v[8];
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
@@ -305,7 +310,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void head_rows_kernel(const HeadAr
   if (col0 < a.V) {
     float* o = logits + (lane & 15) * LD + col0 + 4 * (lane >> 4);
 #pragma unroll
-    for (int n = 0; n < NB; ++n) *reinterpret_cast<f32x4*>(o + 16 * n) = acc[n] * a.scale2;
+    for (int n = 0; n < NB; ++n) *reinterpret_cast<f32x4*>(o + 16 * n) = acc[n];
   }
   __syncthreads();
   constexpr int J = kRowsVocab / 512;  // pieces of eight columns of a lane
@@ -330,17 +335,17 @@ __global__ __launch_bounds__(64 * kRowsWaves) void head_rows_kernel(const HeadAr
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int q = 0; q < 8; ++q) sum += __builtin_amdgcn_exp2f(v[j][q] - at);
+      for (int q = 0; q < 8; ++q) sum += __builtin_amdgcn_exp2f((v[j][q] - at) * a.scale2);
     sum = lanes_sum<64>(sum);
-    const float lse = row_end(rl, row, lane, true, top + __builtin_amdgcn_logf(sum), t, [&](int e) {
+    const RowLse lse = row_end(rl, row, lane, true, RowLse{top, __builtin_amdgcn_logf(sum)}, t, [&](int e) {
       return x[DISTILL ? a.index[row * a.top + e] : (int)t];
     });
     if (a.keep == 0) continue;
-    const bool live = lse != __builtin_inff();  // a row that does not count has none
+    const bool live = lse.live();  // a row that does not count has none
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int q = 0; q < 8; ++q) v[j][q] = live ? __builtin_amdgcn_exp2f(v[j][q] - lse) : 0.f;
+      for (int q = 0; q < 8; ++q) v[j][q] = live ? __builtin_amdgcn_exp2f(lse.log2_p(v[j][q], a.scale2)) : 0.f;
     if constexpr (DISTILL) {
       // through LDS: a lane takes a run of equal indexes
 #pragma unroll

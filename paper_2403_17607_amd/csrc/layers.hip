@@ -63,7 +63,7 @@ DenseWs dense_ws(int64_t M, int64_t K, int64_t N, int mode) {
 
 struct HeadWs {
   HeadPlan plan;
-  size_t lse2, row_loss, alpha, ok, part, pick, index, q, start, P, ref, acc, partial, total;
+  size_t lse, row_loss, alpha, ok, part, pick, index, q, start, P, ref, acc, partial, total;
   int keys;
   int64_t ldp;
 };
@@ -77,7 +77,7 @@ HeadWs head_ws(int64_t M, int64_t D, int64_t V, int top, int mode, bool teacher)
     o = round_up(o + bytes, 256);
     return at;
   };
-  w.lse2 = take((size_t)M * 4);
+  w.lse = take((size_t)M * 8);
   w.row_loss = take((size_t)M * 4);
   w.alpha = take(4);
   w.part = take((size_t)w.plan.parts * M * 8);
@@ -134,7 +134,7 @@ int run_head(bool distill, HeadArgs a, RowLossArgs r, const HeadWs& w, uint8_t* 
   const auto launch = distill ? launch_head_distill : launch_head_ce;
   a.pick = reinterpret_cast<float*>(ws + w.pick);
   a.partial = reinterpret_cast<f32x2*>(ws + w.part);
-  a.lse2 = reinterpret_cast<const float*>(ws + w.lse2);
+  a.lse = reinterpret_cast<const f32x2*>(ws + w.lse);
   a.mt = w.plan.mt;
   a.nt = w.plan.nt;
   a.runs = w.plan.runs;
@@ -152,7 +152,8 @@ int run_head(bool distill, HeadArgs a, RowLossArgs r, const HeadWs& w, uint8_t* 
   r.pick = a.pick;
   r.M = M;
   r.V = V;
-  r.lse2 = reinterpret_cast<float*>(ws + w.lse2);
+  r.lse = reinterpret_cast<f32x2*>(ws + w.lse);
+  r.scale2 = a.scale2;
   if (!r.row_loss) r.row_loss = reinterpret_cast<float*>(ws + w.row_loss);
   r.alpha = reinterpret_cast<float*>(ws + w.alpha);
   hipError_t e;

@@ -125,3 +125,31 @@ def test_teacher_logits_of_the_lowest_value(ffmlp, gpu, V, zt, T):
     logits[4, 0], logits[4, 1] = lowest, -lowest
     logits[5] = float("-inf")  # does not count
     distill_on(ffmlp, H, W, index, logits, T)
+
+
+@pytest.mark.parametrize("V", WORDS)
+@pytest.mark.parametrize("at,T", [(1400.0, 1e-4), (22000.0, 1e-3), (1e5, 1e-4), (-1e5, 1e-4), (1e6, 1e-4)])
+def test_distill_of_large_logits(ffmlp, gpu, V, at, T):
+    """Logits / T beyond 2^24, of either sign.  Every row has one largest logit,
+    or two alike, and the next below by far: the softmax is 1, or 1/2 and 1/2."""
+    g = gen(33)
+    M, D = 64, 16
+    step = 2.0 ** math.floor(math.log2(abs(at)) - 6)  # exact in bf16
+    H = torch.zeros(M, D, device="cuda")
+    rows = torch.arange(M, device="cuda")
+    H[rows, rows % (D - 2)] = 1
+    W = torch.full((D, V), math.floor(at / step) * step, device="cuda")
+    best, second = torch.randint(0, V // 2, (D,), generator=g, device="cuda"), torch.randint(V // 2, V, (D,), generator=g, device="cuda")
+    f = torch.arange(D, device="cuda")
+    W -= step * torch.randint(1, 4, (D, V), generator=g, device="cuda")
+    W[f, best] = math.floor(at / step) * step
+    W[f[::2], second[::2]] = math.floor(at / step) * step
+    H, W = H.to(BF), W.to(BF)
+    l = H.double() @ W.double()
+    top = l.amax(1, keepdim=True)
+    assert step / T > 100
+    p = (l == top).double()
+    p = p / p.sum(1, keepdim=True)
+    index = torch.randint(0, V, (M, 1), generator=g, device="cuda")
+    index[::3, 0] = best[rows[::3] % (D - 2)]
+    distill_on(ffmlp, H, W, index, torch.zeros(M, 1, device="cuda"), T, exact_p=p)
