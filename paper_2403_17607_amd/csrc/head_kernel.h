@@ -14,8 +14,11 @@
 // as bf16, a piece of the vocabulary at a time.  For the first piece the same
 // pass stores 2^((x - r) c + 15) as fp16, r the largest product of the row's
 // columns in a wave's tile, and head_scale_kernel turns that into P in place once
-// m and ls are known.  fp16 up to 2^15: its rounding (2^-12 relative, at most 2^-40 of a
-// probability in absolute terms) does not add to that of P (2^-9).  The logits
+// m and ls are known.  fp16 up to 2^15: half a step is 2^-11 of a value, or
+// 2^-40 of the tile's largest, and P's own rounding to bf16 is 2^-8 of it, so a
+// word outside the target distribution is rounded twice, the second time eight
+// times as coarsely; in it, p is worked out again in fp32 from the word's product
+// and P is rounded once, as everywhere in later pieces.  The logits
 // of later pieces are recomputed by head_prob_kernel.  q is sparse:
 // the one target of a row, or the teacher's top entries sorted by index, with
 // a table of where each block of 128 columns begins in a row's list.
@@ -229,11 +232,17 @@ __global__ __launch_bounds__(256) void head_scale_kernel(const HeadArgs a, const
       const float e = (float)__builtin_bit_cast(_Float16, (uint16_t)(u[q / 2] >> (16 * (q & 1))));
       v[q] = live ? e * f : 0.f;
     }
+    // where q is taken off, p comes from the entry's product itself: with p near q
+    // the fp16 rounding would be most of what is left
     head_hits<DISTILL>(a, row, c & ~(kHeadKey - 1), kHeadKey, [&](int at, int e) {
       const int k = at - (c & (kHeadKey - 1));
-      const float w = DISTILL ? a.q[row * a.top + e] : 1.f;
+      if (k < 0 || k >= 8) return;
+      const int64_t i = row * a.top + e;
+      const float w = DISTILL ? a.q[i] : 1.f;
+      const float p = live ? __builtin_amdgcn_exp2f(lse.log2_p(a.pick[i], a.scale2)) : 0.f;
+      const bool again = DISTILL && e > 0 && a.index[i - 1] == a.index[i];  // equal indexes add up
 #pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] -= k == q ? w : 0.f;
+      for (int q = 0; q < 8; ++q) v[q] = k == q ? (again ? v[q] : p) - w : v[q];
     });
     *reinterpret_cast<u32x4*>(p) = pack8_bf16(v);
   }

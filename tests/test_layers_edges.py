@@ -153,3 +153,25 @@ def test_distill_of_large_logits(ffmlp, gpu, V, at, T):
     index = torch.randint(0, V, (M, 1), generator=g, device="cuda")
     index[::3, 0] = best[rows[::3] % (D - 2)]
     distill_on(ffmlp, H, W, index, torch.zeros(M, 1, device="cuda"), T, exact_p=p)
+
+
+@pytest.mark.parametrize("V", WORDS)
+@pytest.mark.parametrize("gt", [F32, BF])
+@pytest.mark.parametrize("apart", [0.01, 0.3])
+def test_distill_of_a_student_near_its_teacher(ffmlp, gpu, V, gt, apart):
+    """p is near q: what is left of p - q is rounded once, to bf16."""
+    g = gen(34)
+    M, D, top, T = 300, 64, 48, 2.0
+    H, W = randn(g, M, D), randn(g, D, V, std=2 / math.sqrt(D))
+    words = 101 + torch.arange(top, device="cuda") + 3 * (torch.arange(top, device="cuda") > 30)
+    H[:, 0] = 1
+    W[0] = -60.0
+    W[0, words] = 0.0
+    l = (H.double() @ W.double())[:, words]
+    logits = (l + apart * T * torch.randn(M, top, generator=g, device="cuda")).float()
+    perm = torch.rand(M, top, generator=g, device="cuda").argsort(1)
+    distill_on(ffmlp, H, W, words[perm], logits.gather(1, perm), T, gt)
+    # one word twice: its probabilities add up
+    index = words[perm].clone()
+    index[:, 5] = index[:, 9]
+    distill_on(ffmlp, H, W, index, logits.gather(1, perm), T, gt)
