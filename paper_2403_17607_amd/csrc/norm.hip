@@ -498,8 +498,9 @@ __global__ __launch_bounds__(256) void norm_cols_long_kernel(const NormArgs a) {
 
 namespace {
 
-// Workgroups of a pass over rows: a launch has fewer than 2^32 threads.
-unsigned norm_grid(int64_t blocks) { return (unsigned)(blocks < (1 << 23) ? blocks : 1 << 23); }
+// Workgroups of a pass over rows: a launch has fewer than 2^32 threads, whatever a
+// workgroup's are (1024 at most); the kernels go on to further rows by themselves.
+unsigned norm_grid(int64_t blocks) { return (unsigned)(blocks < (1 << 21) ? blocks : 1 << 21); }
 
 template <typename F>
 hipError_t by_types(bool a32, bool b32, F&& f) {

@@ -175,3 +175,24 @@ def test_distill_of_a_student_near_its_teacher(ffmlp, gpu, V, gt, apart):
     index = words[perm].clone()
     index[:, 5] = index[:, 9]
     distill_on(ffmlp, H, W, index, logits.gather(1, perm), T, gt)
+
+
+def test_layer_norm_of_2_23_rows(ffmlp, gpu):
+    """Rows of 512 threads each, as many as make a launch of 2^32 threads."""
+    M, N = 1 << 23, 2049
+    X = torch.empty(M, N, dtype=BF, device="cuda")
+    g = gen(35)
+    some = randn(g, 4099, N)  # rows m and m + 4099 are alike
+    for r in range(0, M, 4099 * 64):
+        n = min(4099 * 64, M - r)
+        X[r:r + n] = some.repeat(64, 1)[:n]
+    want = ffmlp.LayerNorm(N).forward(some)
+    x = some.double()
+    ref = (x - x.mean(1, keepdim=True)) / (x.var(1, unbiased=False, keepdim=True) + 1e-5).sqrt()
+    close(want, ref, (HALF[BF] + 200 * U) * ref.abs() + 200 * U, "Y")
+    stats = torch.empty(M, 2, device="cuda")
+    assert ffmlp.LayerNorm(N).forward(X, Y=X, stats=stats) is X
+    for r in range(0, M, 4099 * 64):
+        n = min(4099 * 64, M - r)
+        assert torch.equal(X[r:r + n], want.repeat(64, 1)[:n])
+    assert torch.equal(stats[:4099], stats[-(M % 4099) - 4099:][:4099]) and torch.isfinite(stats).all()
