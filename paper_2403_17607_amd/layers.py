@@ -161,8 +161,8 @@ class LayerNorm(_Layer):
         lddy = _matrix(dY, "dY", M, n, _TYPES, dev)
         _base._require(stats, "stats", torch.float32, shape=(M, 2), device=dev)
         dX, lddx = _out(dX, "dX", M, n, dtype or X.dtype, dev)
-        dgamma = torch.empty(n, device=dev) if dgamma is None else dgamma
-        dbeta = torch.empty(n, device=dev) if dbeta is None else dbeta
+        dgamma = torch.empty(n, dtype=torch.float32, device=dev) if dgamma is None else dgamma
+        dbeta = torch.empty(n, dtype=torch.float32, device=dev) if dbeta is None else dbeta
         _run(
             _base.lib().mlp_layer_norm_backward, dev, X.data_ptr(), _TYPES[X.dtype], ldx, _vector(gamma, "gamma", n, dev), stats.data_ptr(), dY.data_ptr(),
             _TYPES[dY.dtype], lddy, dX.data_ptr(), _TYPES[dX.dtype], lddx, _vector(dgamma, "dgamma", n, dev),
@@ -234,7 +234,7 @@ class Dense(_Layer):
         elif dX is not None:
             raise ValueError("dX was given, but input_gradient is False")
         dW, lddw = _out(dW, "dW", k, n, dtype, dev)
-        db = torch.empty(n, device=dev) if db is None else db
+        db = torch.empty(n, dtype=torch.float32, device=dev) if db is None else db
         L = _base.lib()
         _run(
             L.mlp_dense_backward, dev, X.data_ptr(), ldx, W.data_ptr(), ldw, self.activation, None if stash is None else stash.data_ptr(),
@@ -267,7 +267,7 @@ class SoftmaxHead(_Layer):
         ldw = _matrix(W, "W", d, v, device=dev)
         args = extra(M, dev)
         if loss is None:
-            loss = torch.empty(1, device=dev)
+            loss = torch.empty(1, dtype=torch.float32, device=dev)
         _base._require(loss, "loss", torch.float32, shape=(1,), device=dev)
         lddh, lddw, pH, pW, tH, tW = d, v, None, None, 0, 0
         if grads:

@@ -196,3 +196,23 @@ def test_layer_norm_of_2_23_rows(ffmlp, gpu):
         n = min(4099 * 64, M - r)
         assert torch.equal(X[r:r + n], want.repeat(64, 1)[:n])
     assert torch.equal(stats[:4099], stats[-(M % 4099) - 4099:][:4099]) and torch.isfinite(stats).all()
+
+
+def test_default_dtype_of_the_program(ffmlp, gpu):
+    """Outputs that the layers allocate are fp32 whatever torch's default is."""
+    ln, de, he = ffmlp.LayerNorm(32), ffmlp.Dense(32, 24), ffmlp.SoftmaxHead(32, 50)
+    g = gen(36)
+    X, W, Wh = randn(g, 6, 32), randn(g, 32, 24), randn(g, 32, 50)
+    stats = torch.empty(6, 2, dtype=F32, device="cuda")
+    t = torch.zeros(6, dtype=torch.int64, device="cuda")
+    old = torch.get_default_dtype()
+    try:
+        for d in (torch.float64, torch.bfloat16):
+            torch.set_default_dtype(d)
+            ln.forward(X, stats=stats)
+            _, dg, db = ln.backward(X, None, stats, X, ln.workspace(6))
+            _, _, b = de.backward(W, X, randn(g, 6, 24), de.workspace(6))
+            loss = he.cross_entropy(Wh, X, t, he.workspace(6))
+            assert dg.dtype == db.dtype == b.dtype == loss.dtype == F32
+    finally:
+        torch.set_default_dtype(old)
