@@ -105,12 +105,20 @@ def _run(fn, dev, *args) -> None:
 
 
 class _Layer:
-    _need = (None, 0)  # the last workspace size asked for, with its arguments
+    # the last workspace size asked for, with its arguments; that of forward calls
+    # apart, so that a training step's two sides do not replace each other's
+    _need = (None, 0)
+    _need_infer = (None, 0)
 
     def _ws_bytes(self, *key) -> int:
-        need = self._need  # read once: other threads may set it
+        infer = key[1:2] == (_base.MLP_MODE_INFER,)
+        need = self._need_infer if infer else self._need  # read once: other threads may set it
         if need[0] != key:
-            self._need = need = (key, self.workspace_bytes(*key))
+            need = (key, self.workspace_bytes(*key))
+            if infer:
+                self._need_infer = need
+            else:
+                self._need = need
         return need[1]
 
     def workspace_bytes(self, M: int, mode: int = _base.MLP_MODE_TRAIN) -> int:

@@ -83,3 +83,20 @@ def test_a_workspace_size_is_that_of_its_own_call(ffmlp):
             return self.mine if self.reads == 1 else ((1, ffmlp.MLP_MODE_INFER, 1), 0)
 
     assert Racing(16, 32)._ws_bytes(8, ffmlp.MLP_MODE_TRAIN, 1) == 12345
+
+
+def test_the_two_sides_of_a_step_keep_their_workspace_sizes(ffmlp):
+    """A forward call's size does not replace the backward call's."""
+    asked = []
+
+    class Counting(ffmlp.Dense):
+        def workspace_bytes(self, M, mode=ffmlp.MLP_MODE_TRAIN):
+            asked.append((M, mode))
+            return super().workspace_bytes(M, mode)
+
+    d = Counting(512, 512, "gelu")
+    for _ in range(3):
+        infer, train = d._ws_bytes(64, ffmlp.MLP_MODE_INFER), d._ws_bytes(64)
+        assert infer == d.workspace_bytes(64, ffmlp.MLP_MODE_INFER) and train == d.workspace_bytes(64)
+    # three times by the test itself, once by the layer
+    assert asked.count((64, ffmlp.MLP_MODE_INFER)) == 4 and asked.count((64, ffmlp.MLP_MODE_TRAIN)) == 4
