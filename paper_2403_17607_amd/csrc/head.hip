@@ -5,7 +5,14 @@ namespace ffmlp {
 
 namespace {
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-constexpr int64_t kPieceElems = (int64_t)1 << 29;  // P of a piece: 1 GiB
+
+// Logits whose exponentials are kept (as fp16, later P as bf16), and that a piece
+// of P holds: 1 GiB, a bound on memory.  There is no knee in it: what is kept is
+// not computed again.  Steps in ms with 2^27, 2^28, 2^29 and 2^30 of them, hidden
+// size 2048: 16384 rows over 65536 words 14.96, 14.67, 13.81 and 12.19; 8192 over
+// 131072 15.13, 14.52, 13.60 and 12.38; 12000 over 65536 12.48, 11.65, 10.97 and
+// 9.87; hidden size 512, 16384 over 50021 4.18, 4.06, 3.90 and 3.71.
+constexpr int64_t kPieceElems = (int64_t)1 << 29;
 }  // namespace
 
 HeadPlan head_plan(int64_t M, int64_t D, int64_t V) {
@@ -24,8 +31,14 @@ HeadPlan head_plan(int64_t M, int64_t D, int64_t V) {
   p.runs = (int)cdiv(p.nt, p.per_run);
   int64_t cols = kPieceElems / (M > 0 ? M : 1) / 256 * 256;
   if (cols < 1024) cols = 1024;
-  const int64_t pieces = cdiv(V, cols);
-  p.piece = (int)(pieces <= 1 ? V : cdiv(cdiv(V, pieces), 256) * 256);
+  // Where one piece does not do, the first is as large as it may be, so that few
+  // logits too many cost few computed twice (8193 rows of 2048 over 65536 words:
+  // 8.65 ms with equal pieces, 8.11 so).  A power of two of columns would put P's
+  // rows 2^n + 128 bytes apart, where head_scale_kernel loses up to a quarter
+  // (32768 rows over 16384 columns 587 us, over 16128 447); one piece more would
+  // cost as much again.
+  if (V > cols && (cols & (cols - 1)) == 0 && cdiv(V, cols - 256) == cdiv(V, cols)) cols -= 256;
+  p.piece = (int)(V < cols ? V : cols);
   p.pieces = (int)cdiv(V, p.piece);
   const int across = p.large ? GemmLarge::WN : GemmMedium::WN;  // waves that share a row of a tile
   p.parts = p.runs * across;

@@ -100,3 +100,12 @@ def test_the_two_sides_of_a_step_keep_their_workspace_sizes(ffmlp):
         assert infer == d.workspace_bytes(64, ffmlp.MLP_MODE_INFER) and train == d.workspace_bytes(64)
     # three times by the test itself, once by the layer
     assert asked.count((64, ffmlp.MLP_MODE_INFER)) == 4 and asked.count((64, ffmlp.MLP_MODE_TRAIN)) == 4
+
+
+def test_a_piece_is_as_large_as_it_may_be(ffmlp):
+    """Where the logits outgrow one piece by a little, only a little of them is
+    left to further pieces (and computed again): the first keeps its size."""
+    h = ffmlp.SoftmaxHead(64, 40000)
+    whole, more = h.workspace_bytes(13400), h.workspace_bytes(13500)
+    assert 13400 * 40000 < 1 << 29 < 13500 * 40000
+    assert 0.98 * whole < more < 1.05 * whole
