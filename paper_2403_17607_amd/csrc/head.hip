@@ -17,9 +17,11 @@ constexpr int64_t kPieceElems = (int64_t)1 << 29;
 
 HeadPlan head_plan(int64_t M, int64_t D, int64_t V) {
   HeadPlan p{};
-  // One round of workgroups: over 1000 words and 128 of k, 4096 rows take 17 us
-  // against 21 in two passes, 8192 24 against 27, 16384 39 against 36; over 256
-  // of k 17, 28 and 51 against 21, 27 and 39.
+  // One round of workgroups, one to a CU.  Whole calls with gradients in us in one
+  // pass and in two, over 1000 words: 4096 rows of 64 34.2 and 42.8, of 128 35.3 and
+  // 43.3, of 256 41.1 and 46.3; 8192 rows 48.4 and 49.3, 51.4 and 50.6, 62.5 and
+  // 57.0; 16384 rows 69.3 and 62.7, 75.2 and 70.6, 100.1 and 88.2; over 200 words of
+  // 128, 4096 rows 26.0 and 29.9, 6144 33.2 and 33.2, 16384 54.6 and 50.6.
   p.rows = V <= kRowsVocab && D <= kRowsDim && M <= 256 * kRowsTile;
   p.large = cdiv(M, GemmLarge::BM) * cdiv(V, GemmLarge::BN) >= 512;
   p.mt = (int)cdiv(M, p.large ? GemmLarge::BM : GemmMedium::BM);

@@ -145,7 +145,15 @@ int run_head(bool distill, HeadArgs a, RowLossArgs r, const HeadWs& w, uint8_t* 
     a.ldp = w.ldp;
     a.keep = w.plan.piece;
     a.ref = reinterpret_cast<float*>(ws + w.ref);
-    a.chunk = M >= 4096 ? 4096 : 1024;  // few rows: more waves (513 rows, 10007 words: 11 -> 8 us)
+    // Columns of a wave of the scaling pass, each of which merges its row's sums
+    // anew: 4096, halved down to 1024 while fewer than 2048 waves come of it.  Steps
+    // of hidden size 64 in us with 1024, 2048, 4096 and 8192: 16 rows over 131072
+    // words 59.5, 60.4, 61.9 and 65.3; 64 over 65536 62.5, 59.6, 60.8 and 64.3; 256
+    // over 50000 72.0, 66.2, 64.9 and 66.6; 2048 over 131072 726, 700, 707 and 707;
+    // 65536 over 4096 723, 714, 689 and 689; hidden size 200, 513 over 10007 57.7,
+    // 57.6, 59.0 and 63.1.
+    a.chunk = 4096;
+    while (a.chunk > 1024 && M * ((w.plan.piece + a.chunk - 1) / a.chunk) < 2048) a.chunk /= 2;
   }
   r.partial = a.partial;
   r.parts = w.plan.parts;
