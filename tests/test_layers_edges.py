@@ -13,7 +13,7 @@ import math
 import pytest
 import torch
 
-from test_layers import BF, F32, HALF, U, check_guard, close, close_norm, gen, guarded, randn
+from test_layers import BF, F32, HALF, U, check_guard, close, close_norm, gen, guarded, norm_case, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -216,3 +216,130 @@ def test_default_dtype_of_the_program(ffmlp, gpu):
             assert dg.dtype == db.dtype == b.dtype == loss.dtype == F32
     finally:
         torch.set_default_dtype(old)
+
+
+# ------------------------------------------------- more than one round of rows --
+
+@pytest.mark.parametrize("M,N,xt,yt", [(7001, 1000, BF, BF), (2051, 2048, BF, BF), (1101, 3001, BF, F32), (1101, 3000, F32, BF), (601, 5003, F32, BF),
+                                       (523, 8192, BF, BF), (300, 16384, BF, BF), (5001, 400, BF, BF), (70001, 24, BF, F32), (33001, 100, F32, F32), (9001, 250, BF, BF)])
+def test_layer_norm_of_several_rows_per_workgroup(ffmlp, gpu, M, N, xt, yt):
+    """Every way of holding a row, with rows left for a second turn of the
+    backward pass's workgroups and a last turn that is not full."""
+    norm_case(ffmlp, M, N, xt, yt, seed=M + N)
+
+
+@pytest.mark.parametrize("M,N,t", [(40003, 24, BF), (20011, 128, F32), (5001, 400, BF), (7001, 1000, BF), (2051, 2048, BF), (1101, 3001, F32), (601, 5003, BF), (300, 16384, F32)])
+def test_layer_norm_backward_in_place_over_several_rows(ffmlp, gpu, M, N, t):
+    """dX may be dY: the rows asked for ahead are not yet written."""
+    g = gen(41)
+    ln = ffmlp.LayerNorm(N)
+    X, dY, gamma = randn(g, M, N, dtype=t), randn(g, M, N, dtype=t), torch.randn(N, generator=g, device="cuda")
+    stats, ws = torch.empty(M, 2, device="cuda"), ln.workspace(M)
+    ln.forward(X, gamma, stats=stats)
+    dX, dg, db = ln.backward(X, gamma, stats, dY, ws)
+    d2 = dY.clone()
+    _, dg2, db2 = ln.backward(X, gamma, stats, d2, ws, dX=d2)
+    assert torch.equal(d2, dX) and torch.equal(dg2, dg) and torch.equal(db2, db)
+
+
+@pytest.mark.parametrize("N", [40, 100, 1000, 2049, 20001])
+def test_layer_norm_keeps_what_is_not_finite_to_its_row(ffmlp, gpu, N):
+    """A row with an infinity or a NaN is NaN; its neighbours, which share its
+    wave or workgroup, are as without it."""
+    g = gen(42)
+    ln = ffmlp.LayerNorm(N)
+    X, dY = randn(g, 9, N, dtype=F32), randn(g, 9, N, dtype=F32)
+    Xb = X.clone()
+    Xb[2, N // 2], Xb[5, N - 1], Xb[7, 0] = float("inf"), float("nan"), float("-inf")
+    bad = torch.zeros(9, dtype=torch.bool, device="cuda")
+    bad[[2, 5, 7]] = True
+    st, stb = torch.empty(9, 2, device="cuda"), torch.empty(9, 2, device="cuda")
+    Y, Yb = ln.forward(X, stats=st), ln.forward(Xb, stats=stb)
+    assert torch.equal(Y[~bad], Yb[~bad]) and Yb[bad].isnan().all() and stb[bad].isnan().any(1).all()
+    dX, _, db = ln.backward(X, None, st, dY, ln.workspace(9))
+    dXb, dgb, dbb = ln.backward(Xb, None, stb, dY, ln.workspace(9))
+    assert torch.equal(dX[~bad], dXb[~bad]) and dXb[bad].isnan().all() and dgb.isnan().all() and torch.equal(db, dbb)
+
+
+# ------------------------------------------------------------- several pieces --
+
+def pieces_case(ffmlp, M, D, V, T, gt, seed, rows, words):
+    """A step of several pieces, checked at some rows of dH and columns of dW.
+    Lists of 4 within the first, a middle and the last words."""
+    g = gen(seed)
+    H, W = randn(g, M, D), randn(g, D, V, std=2 * T / math.sqrt(D))
+    index = torch.randint(0, V, (M, 4), generator=g, device="cuda")
+    index[:, 1] = (index[:, 0] + V // 2) % V
+    index[::5, 2] = -1
+    index[3::50] = -1
+    logits = torch.randn(M, 4, generator=g, device="cuda")
+    head = ffmlp.SoftmaxHead(D, V)
+    ws = head.workspace(M, top=4)
+    ws.fill_(255)
+    rl = torch.empty(M, device="cuda")
+    dH, dW, loss = head.distill_step(W, H, index, logits, ws, temperature=T, row_loss=rl, dtype=gt)
+    q, e_q, live = teacher64(index, logits, T)
+    n, w = int(live.sum()), W.double()
+    a = T / n
+    h = H[rows].double()
+    l = h @ w / T
+    e_l = (D + 8) * U * (h.abs() @ w.abs()) / T
+    lse = torch.logsumexp(l, 1, keepdim=True)
+    p = torch.exp(l - lse) * live[rows][:, None]
+    ix = index[rows].clamp_min(0)
+    P = p.scatter_add(1, ix, -q[rows])
+    e_P = p * (e_l + e_l.amax(1, keepdim=True) + 56 * U + 2.0 ** -11) + 2.0 ** -40
+    e_P = e_P.scatter_add(1, ix, e_q[rows]) + HALF[BF] * P.abs()
+    ref, s = a * (P @ w.t()), a * (P.abs() @ w.abs().t())
+    close(dH[rows], ref, a * (e_P @ w.abs().t()) + (V + 16) * U * s + HALF[gt] * (ref.abs() + HALF[BF] * s) + 1e-14, "dH")
+    close_norm(dH[rows], ref, a * ((e_P.square() @ w.square().t()).sum().sqrt()).item() + math.sqrt(V + 16) * U * s.norm().item()
+               + HALF[gt] * ref.norm().item() + 1e-14, "dH norm")
+    # columns of dW: over all rows, some at a time
+    ref, s, e1, e2 = (torch.zeros(D, len(words), dtype=torch.float64, device="cuda") for _ in range(4))
+    wc = w[:, words]
+    for r in range(0, M, 4096):
+        h = H[r:r + 4096].double()
+        lse = torch.cat([torch.logsumexp(h[k:k + 512] @ w / T, 1, keepdim=True) for k in range(0, len(h), 512)])
+        e_l = (D + 8) * U * (h.abs() @ w.abs().amax(1))[:, None] / T
+        p = torch.exp(h @ wc / T - lse) * live[r:r + 4096, None]
+        hit = (index[r:r + 4096, :, None] == words).double()
+        P = p - (q[r:r + 4096, :, None] * hit).sum(1)
+        e_P = p * (2 * e_l + 56 * U + 2.0 ** -11) + 2.0 ** -40 + (e_q[r:r + 4096, :, None] * hit).sum(1) + HALF[BF] * P.abs()
+        ref += a * (h.t() @ P)
+        s += a * (h.abs().t() @ P.abs())
+        e1 += a * (h.abs().t() @ e_P)
+        e2 += a * a * (h.square().t() @ e_P.square())
+    close(dW[:, words], ref, e1 + (M + 8) * U * s + HALF[gt] * (ref.abs() + HALF[BF] * s) + 1e-14, "dW")
+    close_norm(dW[:, words], ref, e2.sum().sqrt().item() + math.sqrt(M + 8) * U * s.norm().item() + HALF[gt] * ref.norm().item() + 1e-14, "dW norm")
+    assert torch.isfinite(dH).all() and torch.isfinite(dW).all() and torch.isfinite(loss).all() and (dH[~live] == 0).all()
+
+
+@pytest.mark.parametrize("gt", [F32, BF])
+def test_three_pieces(ffmlp, gpu, gt):
+    """2^20 rows: pieces of 1024 words, the middle one added to and written."""
+    M, V = 1 << 20, 2500
+    pieces_case(ffmlp, M, 8, V, 1.5, gt, 43, torch.arange(0, M, 1709, device="cuda"),
+                torch.tensor([0, 1, 500, 1023, 1024, 1025, 1500, 2047, 2048, 2300, 2499], device="cuda"))
+
+
+def test_pieces_of_a_wide_hidden_size(ffmlp, gpu):
+    """Two pieces and a rest behind them, at a hidden size of several steps."""
+    M, D, V = 12345, 328, 90001
+    assert M * V > 1 << 30
+    words = torch.cat([torch.arange(0, V, 5003), torch.tensor([43263, 43264, 86527, 86528, V - 1])]).to("cuda")
+    pieces_case(ffmlp, M, D, V, 2.0, F32, 44, torch.arange(0, M, 63, device="cuda"), words)
+
+
+# ---------------------------------------------------------------- error norms --
+
+@pytest.mark.parametrize("M,D,V", [(300, 256, 1000), (300, 300, 1000), (257, 130, 5003), (2050, 64, 4101), (1500, 512, 8192)])
+@pytest.mark.parametrize("gt", [F32, BF])
+def test_losses_in_the_norm(ffmlp, gpu, M, D, V, gt):
+    """Errors of dH and dW in the norm, where independent roundings do not add
+    up as their absolute values do."""
+    g = gen(45)
+    H, W = randn(g, M, D), randn(g, D, V, std=2 / math.sqrt(D))
+    index = torch.rand(M, V, generator=g, device="cuda").topk(9, 1).indices
+    index[::6, 4:] = -1
+    distill_on(ffmlp, H, W, index, 2 * torch.randn(M, 9, generator=g, device="cuda"), 1.0, gt)
+    distill_on(ffmlp, H, W, index[:, :1].contiguous(), torch.zeros(M, 1, device="cuda"), 1.0, gt)
