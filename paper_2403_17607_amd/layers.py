@@ -212,7 +212,7 @@ class Dense(_Layer):
         ldx, dev = _matrix(X, "X", M, k), X.device
         ldw = _matrix(W, "W", k, n, device=dev)
         if dtype is None:
-            dtype = torch.bfloat16 if residual is None else residual.dtype
+            dtype = residual.dtype if isinstance(residual, torch.Tensor) else torch.bfloat16
         Y, ldy = _out(Y, "Y", M, n, dtype, dev)
         ldr = 0 if residual is None else _matrix(residual, "residual", M, n, (Y.dtype,), dev)
         if stash is not None:

@@ -343,3 +343,10 @@ def test_losses_in_the_norm(ffmlp, gpu, M, D, V, gt):
     index[::6, 4:] = -1
     distill_on(ffmlp, H, W, index, 2 * torch.randn(M, 9, generator=g, device="cuda"), 1.0, gt)
     distill_on(ffmlp, H, W, index[:, :1].contiguous(), torch.zeros(M, 1, device="cuda"), 1.0, gt)
+
+
+def test_residual_must_be_a_tensor(ffmlp, gpu):
+    de = ffmlp.Dense(32, 24)
+    g = gen(46)
+    with pytest.raises(ValueError, match="residual"):
+        de.forward(randn(g, 32, 24), randn(g, 4, 32), residual=1.0)
