@@ -326,10 +326,11 @@ int mlp_dense_backward(const uint16_t* X, int64_t ldx, const uint16_t* W,
 size_t mlp_head_workspace_bytes(int64_t M, int64_t D, int64_t V, int top,
                                 int mode);
 
-/* Softmax cross entropy of the logits L = H W, which are never stored whole:
+/* Softmax cross entropy of the logits L = H W, which are not stored themselves:
  * the loss keeps a running maximum and sum per row, the gradients take the
- * vocabulary in pieces of at most 1 GiB of 16-bit values (or 1024 columns), a
- * later piece's logits being computed again.
+ * probabilities of the vocabulary in pieces of at most 1 GiB of 16-bit values (or
+ * 1024 columns).  The first piece holds all of them where they fit; a later
+ * piece's logits are computed again.
  *   H       bf16 [M][D];  W  bf16 [D][V].
  *   target  int64 [M], 8-byte aligned: 0 .. V - 1, or ignore_index for a row
  *           that does not count.  Any other value makes the loss (and the
@@ -338,8 +339,10 @@ size_t mlp_head_workspace_bytes(int64_t M, int64_t D, int64_t V, int top,
  *           log sum exp L - L[target] (0 if none does).
  *   row_loss  fp32 [M] or NULL: the same per row, 0 for rows that do not count.
  *   dH      [M][D], dW [D][V], bf16 or fp32 each: gradients of the mean loss;
- *           both or neither (NULL).  softmax - target is rounded to bf16 once
- *           before the two products.  A row that does not count gives zeros
+ *           both or neither (NULL).  The product's operand softmax - target is
+ *           bf16, rounded from fp32 where the target is; elsewhere the softmax
+ *           may have passed through fp16 (2^-11 of it) before that rounding
+ *           (2^-8).  A row that does not count gives zeros
  *           to dH; its H has to be finite for dW, as in any product.
  * 0 <= M <= 2^24. */
 int mlp_cross_entropy(const uint16_t* H, int64_t ldh, const uint16_t* W,
@@ -355,10 +358,12 @@ int mlp_cross_entropy(const uint16_t* H, int64_t ldh, const uint16_t* W,
  *   index   int64 [M][top], contiguous: a negative index is no entry, one past
  *           the vocabulary makes loss and gradients NaN; an index may occur
  *           twice (its probabilities add up).  A row without an entry (or
- *           with logits of -inf alone) does not count.
+ *           with logits of -inf alone) does not count.  Probabilities below
+ *           2^-126 are 0.
  *   logits  [M][top], bf16 or fp32, contiguous.
  *   temperature  1e-4 .. 1e4.
- * Other arguments as for mlp_cross_entropy. */
+ * Other arguments as for mlp_cross_entropy, the row's entries in the target's
+ * place. */
 int mlp_distill(const uint16_t* H, int64_t ldh, const uint16_t* W, int64_t ldw,
                 const int64_t* index, const void* logits, int logits_type,
                 int top, float temperature, float* loss, float* row_loss,

@@ -21,6 +21,8 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 //   1024 x 1024 over 1024 (X W): large 25, half 16, medium 10.1, small 8.1
 //   1111 x 771 over 1283 (dZ W^T): medium 13.5, small 10.8; 1111 x 1283 over 771
 //     (X W): medium 10.1, small 12.4
+// The costs are those of aligned rows and bf16 results; where rows start at odd
+// elements or a result is fp32, every tile takes longer, in other proportions.
 struct TileCost {
   int tile, bm, bn, bk, per_cu;
   double alone, shared, rest;
@@ -136,7 +138,7 @@ hipError_t launch_gemm(int form, GemmArgs a, float* partial, hipStream_t s) {
 // them as 16-byte pieces, the wave's 64 / LPR groups take eight consecutive k
 // each, the 16 waves every 16th such block.  Then the groups' sums are added by
 // shuffles and the waves' in order through LDS.  LPR is chosen so that 256
-// workgroups or more share N; those that share the 128 bytes of a line run on
+// workgroups or more share an N of 4096 or more; those that share the 128 bytes of a line run on
 // one chiplet.  4096 x 4096 with GELU: 11.3 us, against 13 of the matrix-core
 // kernel with splits (two launches), which two rows take too.
 template <int LPR>

@@ -1,4 +1,4 @@
-// Losses of the logits H W over a vocabulary, never stored whole.
+// Losses of the logits H W over a vocabulary, which are not stored themselves.
 //
 //   x = H W,  c = log2(e) / T                  (logits / T in base 2: x c)
 //   m = max_v x,  ls = log2 sum_v 2^((x - m) c)
@@ -9,19 +9,19 @@
 // is off by that much overflowed the fp16 below.
 //
 // head_lse_kernel walks a run of column tiles with one row tile and keeps the
-// running maximum and sum of every row in registers, so the logits live only
-// in the matrix cores' results.  The gradients dH = P W^T and dW = H^T P take P
-// as bf16, a piece of the vocabulary at a time.  For the first piece the same
-// pass stores 2^((x - r) c + 15) as fp16, r the largest product of the row's
-// columns in a wave's tile, and head_scale_kernel turns that into P in place once
-// m and ls are known.  fp16 up to 2^15: half a step is 2^-11 of a value, or
-// 2^-40 of the tile's largest, and P's own rounding to bf16 is 2^-8 of it, so a
-// word outside the target distribution is rounded twice, the second time eight
-// times as coarsely; in it, p is worked out again in fp32 from the word's product
-// and P is rounded once, as everywhere in later pieces.  The logits
-// of later pieces are recomputed by head_prob_kernel.  q is sparse:
-// the one target of a row, or the teacher's top entries sorted by index, with
-// a table of where each block of 128 columns begins in a row's list.
+// running maximum and sum of every row in registers; for the loss alone nothing
+// else leaves it.  The gradients dH = P W^T and dW = H^T P take P as bf16, a piece
+// of the vocabulary at a time.  For the first piece the same pass stores
+// 2^((x - r) c + 15) as fp16, r the largest product of the row's columns in a
+// wave's tile, and head_scale_kernel turns that into P in place once m and ls are
+// known.  fp16 up to 2^15: half a step is 2^-11 of a value, or 2^-40 of the tile's
+// largest, and P's own rounding to bf16 is 2^-8 of it, so a word outside the
+// target distribution is rounded twice, the second time eight times as coarsely;
+// in it, p is worked out again in fp32 from the word's product and p - q is rounded
+// once, as everywhere in later pieces, whose products head_prob_kernel computes
+// again.  q is sparse: the one target of a row, or the teacher's top entries
+// sorted by index, with a table of where each block of 128 columns begins in a
+// row's list.
 //
 // 8192 rows of 2048 over 65536 words: head_lse_kernel 2.1 ms (1050 TFLOP/s at
 // 1.7 GHz, the matrix cores 54% busy: bound by power and by what feeds them),

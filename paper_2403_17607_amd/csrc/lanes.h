@@ -8,8 +8,9 @@
 
 namespace ffmlp {
 
-// op(v of this lane, v of the lane whose number differs in bit D), where v is
-// the same in all lanes that differ in bits below D only.
+// op(v of this lane, v of the lane whose number differs in bit D).  Steps of 4 and
+// 8 mirror their lanes, which is the same where lanes that differ in lower bits
+// only hold the same v.
 template <int D, typename F>
 __device__ __forceinline__ float lanes_step(float v, F&& op) {
   const uint32_t x = __float_as_uint(v);
@@ -22,8 +23,9 @@ __device__ __forceinline__ float lanes_step(float v, F&& op) {
     return op(v, __uint_as_float(__builtin_amdgcn_mov_dpp((int)x, ctrl, 0xf, 0xf, true)));
   }
 }
-// Over groups of LANES lanes (a power of two), every lane with the result; from
-// FROM on where lower groups agree already.
+// Over groups of LANES lanes (a power of two), every lane with the result.  With
+// FROM over the lanes that differ in bits FROM .. LANES / 2 only: 16 and 32, which
+// take exactly those lanes, or 1.
 template <int LANES, int FROM = 1, typename F>
 __device__ __forceinline__ float lanes_all(float v, F&& op) {
   if constexpr (FROM < LANES) return lanes_all<LANES, 2 * FROM>(lanes_step<FROM>(v, op), op);

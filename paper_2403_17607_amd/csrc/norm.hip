@@ -24,7 +24,7 @@ template <bool F32> struct Elem { typedef uint16_t type; };
 template <> struct Elem<true> { typedef float type; };
 
 // Sums of K values over the G consecutive threads that hold a row, in a fixed
-// order: within a wave as above, and through LDS (K floats per wave) where they
+// order: within a wave by lanes_sum, and through LDS (K floats per wave) where they
 // are several waves, which all of the workgroup then passes together.
 template <int G, int K>
 __device__ __forceinline__ void row_sum(float (&v)[K], float* lds) {
@@ -371,42 +371,42 @@ __global__ __launch_bounds__(256) void norm_fwd_long_kernel(const NormArgs a) {
   typedef typename Elem<Y32>::type TY;
   __shared__ float lds[8];
   for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
-  const TX* X = static_cast<const TX*>(a.X) + row * a.ldx;
-  TY* Y = static_cast<TY*>(a.Y) + row * a.ldy;
-  float s[1] = {0.f}, v[1] = {0.f}, x[8];
-  for (int c = 8 * threadIdx.x; c < a.N; c += 2048) {
-    load8(X + c, a.N - c, x);
-    float t = 0.f;
+    const TX* X = static_cast<const TX*>(a.X) + row * a.ldx;
+    TY* Y = static_cast<TY*>(a.Y) + row * a.ldy;
+    float s[1] = {0.f}, v[1] = {0.f}, x[8];
+    for (int c = 8 * threadIdx.x; c < a.N; c += 2048) {
+      load8(X + c, a.N - c, x);
+      float t = 0.f;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) t += x[q];
-    s[0] += t;
-  }
-  row_sum<256>(s, lds);
-  const float mean = s[0] / (float)a.N;
-  for (int c = 8 * threadIdx.x; c < a.N; c += 2048) {
-    load8(X + c, a.N - c, x);
-    float t = 0.f;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) t += c + q < a.N ? (x[q] - mean) * (x[q] - mean) : 0.f;
-    v[0] += t;
-  }
-  row_sum<256>(v, lds);
-  const float rstd = 1.f / __builtin_sqrtf(v[0] / (float)a.N + a.eps);
-  if (a.stats && threadIdx.x == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * row) = f32x2{mean, rstd};
-  for (int c = 8 * threadIdx.x; c < a.N; c += 2048) {
-    const int n = a.N - c;
-    float g[8], b[8];
-    load8(X + c, n, x);
-    if (a.gamma) load8(a.gamma + c, n, g);
-    if (a.beta) load8(a.beta + c, n, b);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      x[q] = (x[q] - mean) * rstd;
-      if (a.gamma) x[q] *= g[q];
-      if (a.beta) x[q] += b[q];
+      for (int q = 0; q < 8; ++q) t += x[q];
+      s[0] += t;
     }
-    store8(Y + c, n, x);
-  }
+    row_sum<256>(s, lds);
+    const float mean = s[0] / (float)a.N;
+    for (int c = 8 * threadIdx.x; c < a.N; c += 2048) {
+      load8(X + c, a.N - c, x);
+      float t = 0.f;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) t += c + q < a.N ? (x[q] - mean) * (x[q] - mean) : 0.f;
+      v[0] += t;
+    }
+    row_sum<256>(v, lds);
+    const float rstd = 1.f / __builtin_sqrtf(v[0] / (float)a.N + a.eps);
+    if (a.stats && threadIdx.x == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * row) = f32x2{mean, rstd};
+    for (int c = 8 * threadIdx.x; c < a.N; c += 2048) {
+      const int n = a.N - c;
+      float g[8], b[8];
+      load8(X + c, n, x);
+      if (a.gamma) load8(a.gamma + c, n, g);
+      if (a.beta) load8(a.beta + c, n, b);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        x[q] = (x[q] - mean) * rstd;
+        if (a.gamma) x[q] *= g[q];
+        if (a.beta) x[q] += b[q];
+      }
+      store8(Y + c, n, x);
+    }
   }
 }
 
@@ -416,42 +416,42 @@ __global__ __launch_bounds__(256) void norm_bwd_long_kernel(const NormArgs a) {
   typedef typename Elem<DY32>::type TD;
   __shared__ float lds[8];
   for (int64_t row = blockIdx.x; row < a.M; row += gridDim.x) {
-  const TX* X = static_cast<const TX*>(a.X) + row * a.ldx;
-  const TD* D = static_cast<const TD*>(a.dY) + row * a.lddy;
-  const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
-  float s[2] = {0.f, 0.f}, x[8], d[8], g[8];
-  auto load = [&](int c) {
-    const int n = a.N - c;
-    load8(X + c, n, x);
-    load8(D + c, n, d);
-    if (a.gamma) load8(a.gamma + c, n, g);
+    const TX* X = static_cast<const TX*>(a.X) + row * a.ldx;
+    const TD* D = static_cast<const TD*>(a.dY) + row * a.lddy;
+    const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + 2 * row);
+    float s[2] = {0.f, 0.f}, x[8], d[8], g[8];
+    auto load = [&](int c) {
+      const int n = a.N - c;
+      load8(X + c, n, x);
+      load8(D + c, n, d);
+      if (a.gamma) load8(a.gamma + c, n, g);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      x[q] = q < n ? (x[q] - st[0]) * st[1] : 0.f;
-      if (a.gamma) d[q] *= g[q];
+      for (int q = 0; q < 8; ++q) {
+        x[q] = q < n ? (x[q] - st[0]) * st[1] : 0.f;
+        if (a.gamma) d[q] *= g[q];
+      }
+    };
+    for (int c = 8 * threadIdx.x; c < a.N; c += 2048) {
+      load(c);
+      float t1 = 0.f, t2 = 0.f;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        t1 += d[q];
+        t2 += d[q] * x[q];
+      }
+      s[0] += t1;
+      s[1] += t2;
     }
-  };
-  for (int c = 8 * threadIdx.x; c < a.N; c += 2048) {
-    load(c);
-    float t1 = 0.f, t2 = 0.f;
+    row_sum<256>(s, lds);
+    s[0] /= (float)a.N;
+    s[1] /= (float)a.N;
+    for (int c = 8 * threadIdx.x; c < a.N; c += 2048) {
+      load(c);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      t1 += d[q];
-      t2 += d[q] * x[q];
+      for (int q = 0; q < 8; ++q) d[q] = st[1] * (d[q] - s[0] - x[q] * s[1]);
+      if (a.dx_fp32) store8(static_cast<float*>(a.dX) + row * a.lddx + c, a.N - c, d);
+      else store8(static_cast<uint16_t*>(a.dX) + row * a.lddx + c, a.N - c, d);
     }
-    s[0] += t1;
-    s[1] += t2;
-  }
-  row_sum<256>(s, lds);
-  s[0] /= (float)a.N;
-  s[1] /= (float)a.N;
-  for (int c = 8 * threadIdx.x; c < a.N; c += 2048) {
-    load(c);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) d[q] = st[1] * (d[q] - s[0] - x[q] * s[1]);
-    if (a.dx_fp32) store8(static_cast<float*>(a.dX) + row * a.lddx + c, a.N - c, d);
-    else store8(static_cast<uint16_t*>(a.dX) + row * a.lddx + c, a.N - c, d);
-  }
   }
 }
 
