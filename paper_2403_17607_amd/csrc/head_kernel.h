@@ -25,7 +25,7 @@
 //
 // 8192 rows of 2048 over 65536 words: head_lse_kernel 2.1 ms (1050 TFLOP/s at
 // 1.7 GHz, the matrix cores 54% busy: bound by power and by what feeds them),
-// head_scale_kernel 0.44 ms (5.3 TB/s), the gradients' products 1.94 and 1.90 ms.
+// head_scale_kernel 0.44 ms (5.3 TB/s), the gradients' products 1.93 and 1.89 ms.
 // Computing the logits again instead of the scaling pass would take 2.1 ms.
 #pragma once
 
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(TL::NTHR, 2) void head_prob_kernel(const HeadArgs a
 }
 
 // P of the first piece from what head_lse_kernel kept of it, in place; bound by
-// memory (4096 rows of 32768: 117 us, 4.6 TB/s).  Wave
+// memory (4096 rows of 32768, lists of 32: 120 us, 4.5 TB/s).  Wave
 // w of block (x, y): row 4 x + w, columns `chunk` y on, 512 at a time; G: columns
 // per reference.  Each wave merges its row's sums itself and those of y = 0 write
 // the row's loss: one launch less.
