@@ -256,9 +256,9 @@ class SoftmaxHead(_Layer):
     """Losses of the logits H W, W bf16 [dim, vocab], over a vocabulary.  The
     logits are not stored: the loss alone keeps two sums per row and run of
     columns, the ..._step calls the probabilities of a piece of the vocabulary
-    in 16 bits, up to 1 GiB in the workspace.  These also return the gradients
-    of the mean loss, as train_step does; dH is what a net that made H takes as
-    its dY."""
+    in 16 bits, up to 1 GiB (or 1024 columns) in the workspace.  These also
+    return the gradients of the mean loss, as train_step does; dH is what a net
+    that made H takes as its dY."""
 
     def __init__(self, dim: int, vocab: int):
         self.dim, self.vocab = _dim(dim, "dim"), _dim(vocab, "vocab")
